@@ -345,6 +345,107 @@ int pie_prefill_attention(pie_pool *pool, int32_t layer, const void *q, void *ou
                           int32_t max_blocks_per_seq, const int32_t *ctx_lens_dev, const int32_t *q_offsets_dev,
                           const int32_t *ctx_lens_host, const int32_t *q_offsets_host, int32_t n_seqs, float scale);
 
+/* ---- rotary positions, fused with the cache write --------------------------------------------------------------
+ * (No counterpart in the paper, whose engine takes rotated q and k for granted.)  A head's first rotary_dim elements are
+ * rotary_dim / 2 pairs; pair i of a token is turned by the angle positions[axis of the pair][token] * inv_freq[i]:
+ *     (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ * The elements behind rotary_dim stay as they are.  One axis is the usual rotary embedding; images and video give every
+ * token a time, a height and a width and share the pairs out among them (consecutive sections, in turn, or any other way:
+ * pair_axis says which).  Pair i is elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) where adjacent != 0.
+ * pair_axis, inv_freq: host, rotary_dim / 2 entries each; axes are 0 .. 3, and a call's positions have one row per axis up
+ * to the largest one named.  Frequencies are radians per position (their own scaling for long contexts included), amplitude
+ * what such schemes multiply the cosine and the sine by (1 otherwise).  Angles are formed in 64-bit fixed point, in turns:
+ * a position of any size, negative ones too, keeps its fraction to 2^-32 of a turn.
+ * Can be called again at any time; calls already enqueued keep the setting they were made with.
+ * PIE_ERR_INVALID: a null pointer, an axis outside 0 .. 3, a frequency or amplitude that is not finite, amplitude <= 0,
+ * rotary_dim <= 0 or above head_dim.  PIE_ERR_UNSUPPORTED: rotary_dim not a multiple of 16. */
+#define PIE_ROPE_MAX_AXES 4
+int pie_set_rope(pie_pool *pool, int32_t rotary_dim, const int32_t *pair_axis, const double *inv_freq, int32_t adjacent,
+                 float amplitude);
+/* The host half of pie_set_rope by itself (needs no GPU): checks its arguments, fills turns[rotary_dim / 2] with the pairs'
+ * frequencies as 2^64-ths of a turn per position (the angle of position p is the low 64 bits of p * turns[i]) and *n_axes
+ * with the number of rows that positions must have. */
+int pie_rope_plan(int32_t head_dim, int32_t rotary_dim, const int32_t *pair_axis, const double *inv_freq, uint64_t *turns,
+                  int32_t *n_axes);
+/* Rotates q and k of n_tokens tokens and writes the rotated k and v into the cache, as pie_kv_write does, in one pass:
+ *   q [n_tokens][n_q_heads][head_dim] -> q_out, k [n_tokens][n_kv_heads][head_dim] -> the cache and, if k_out is not NULL,
+ *   k_out; v (as k) -> the cache.  All in the pool's 16-bit type; the rotation is computed in fp32 and rounded once (an 8-bit
+ *   cache takes E4M3(rotated value / scale) straight from fp32).
+ * q_stride, k_stride, v_stride: elements from a token to the next (0: dense); q, k and v may be slices of one projection's
+ * rows.  q_out and k_out are dense and may be q and k themselves where those are dense.
+ * positions_dev: device int32 [n_axes][n_tokens].  token_seq_dev, token_pos_dev, block_table_dev: as for pie_kv_write - the
+ * token's place in the cache, which need not be its rotary position.
+ * block_table_dev == NULL: nothing is written to the cache (v, token_seq_dev and token_pos_dev are not looked at): for
+ * pie_decode_step, which appends k_out itself.  q or k may be NULL (with its output) where only the other is wanted; k and v
+ * are required with a block table.
+ * A token whose block is not on the GPU, or whose sequence or position is out of range, is rotated but not written, and the
+ * next call that checks the device status word returns PIE_ERR_NOT_RESIDENT / PIE_ERR_INVALID.  Two tokens of one call must
+ * not name the same place.  Enqueued and ordered like pie_kv_write; one token per sequence is the decode step's form.
+ * PIE_ERR_INVALID: before pie_set_rope, a pointer or stride not on a 16-byte boundary, a stride below its row, an output that
+ * overlaps an input otherwise than named above.  PIE_ERR_UNSUPPORTED while the compute stream is being captured: calls on a
+ * pool keep host-side books, which a replayed graph would not. */
+int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out, const void *k, void *k_out, const void *v,
+                      const int32_t *positions_dev, const int32_t *token_seq_dev, const int32_t *token_pos_dev,
+                      int64_t n_tokens, const int32_t *block_table_dev, int32_t max_blocks_per_seq, int32_t n_seqs,
+                      int64_t q_stride, int64_t k_stride, int64_t v_stride);
+
+/* ---- attention over whole prompts (Section 2.1: the prefill stage computes all prompt tokens at once) ---------------
+ * For prompts with nothing cached before them: keys and values are read from k and v as the projection left them, the cache
+ * is not touched (pie_kv_write or pie_rope_kv_write fills it, before or after).  Sequence s owns tokens offsets_host[s] ..
+ * offsets_host[s + 1] - 1 of the packed arrays and each of its tokens attends to its sequence's tokens up to itself:
+ *     out[i][h] = sum_{t <= i} softmax_t(scale * q[i][h] . k[t][kvh]) * v[t][kvh],    kvh = h / (n_q_heads / n_kv_heads)
+ * q: device [n_tokens][n_q_heads][head_dim], k, v: device [n_tokens][n_kv_heads][head_dim] in the pool's 16-bit type (8-bit
+ * pools too: the arrays are 16-bit), tokens q_stride / k_stride / v_stride elements apart (0: dense); out: dense, like q.
+ * Sequences of any length, empty ones too; rows behind the last offset are left as they were.  What a token may not see
+ * cannot reach it, NaN and infinities included.  Scores and sums in fp32, probabilities rounded to the 16-bit type before
+ * they meet the values (each by 2^-9 (bf16) or 2^-12 (fp16) of itself at most, independently: less than the output's own
+ * rounding), out rounded to nearest.
+ * offsets_host: host, n_seqs + 1 entries, first 0, ascending.  PIE_ERR_INVALID: offsets that are not, pointers or strides not
+ * on a 16-byte boundary, a stride below its row, out overlapping an input.  PIE_ERR_UNSUPPORTED while the compute stream is
+ * being captured. */
+int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const void *v, void *out, const int32_t *offsets_host,
+                         int32_t n_seqs, float scale, int64_t q_stride, int64_t k_stride, int64_t v_stride);
+
+/* ---- attention weights and eviction ------------------------------------------------------------------------------
+ * (No counterpart in the paper: a cache that forgets costs neither HBM nor link.)
+ * pie_decode_attention that also adds, for every cached token t < ctx_len of a sequence and every KV head, the weight that
+ * the head group's queries gave it:
+ *     weights[s][kvh][t] += sum over the group's heads h of softmax_t(scale * q[s][h] . k[t])
+ * weights: device fp32 [n_seqs][n_kv_heads][weights_stride]; entries at and behind ctx_len are left as they were (the caller
+ * clears the entry of a new token, or starts from zeros).  The sums are formed in one fixed order: the same bits every time,
+ * wherever the blocks lie.  out and the append are pie_decode_attention's (block_table_host .. v_new may be NULL).  A
+ * context longer than weights_stride: PIE_ERR_INVALID with host lengths; without them the entries beyond are dropped and the
+ * next call returns PIE_ERR_INVALID.  PIE_ERR_UNSUPPORTED while the compute stream is being captured.  The first call on a
+ * pool allocates its score scratch (4 * n_q_heads bytes per token of the pool). */
+int pie_decode_attention_weights(pie_pool *pool, int32_t layer, const void *q, void *out, const int32_t *block_table_dev,
+                                 int32_t max_blocks_per_seq, const int32_t *ctx_lens_dev, const int32_t *block_table_host,
+                                 const int32_t *ctx_lens_host, int32_t n_seqs, float scale, const void *k_new,
+                                 const void *v_new, float *weights, int64_t weights_stride);
+/* Shortens every sequence of more than `budget` cached tokens to `budget` in one layer.  Each KV head keeps, of its own
+ * choice, the newest `recent` tokens and the budget - recent others with the largest weights (equal weights: the lower
+ * position; NaN counts as the smallest), in their old order, moved to positions 0 .. budget - 1; attention goes on over the
+ * shortened sequence with ctx_len = budget (+ new tokens).  Keys are moved as they are stored, so a rotary position stays what
+ * it was.  Sequences of at most `budget` tokens keep everything.
+ * weights: as above (weights_stride entries per row).
+ * dst_block_table_dev (device int32 [n_seqs][dst_max_blocks], logical ids): where the kept tokens go; its blocks must not be
+ * among the source's (a shared prefix stays intact).  NULL: in place, into the first blocks of block_table_dev, which then must
+ * not be shared between sequences.
+ * weights_out (device fp32 [n_seqs][n_kv_heads][weights_out_stride]): entry j receives the weight of the token now at position
+ * j, entries from the new length up to the old one (as far as the stride reaches) become 0.  NULL: in place.
+ * new_lens_dev (device int32 [n_seqs], may be NULL, may be ctx_lens_dev itself): min(ctx, budget).
+ * kept_dev (device int32 [n_seqs][n_kv_heads][budget], may be NULL): the old position of each kept token, -1 behind them.
+ * Every block read or written must be GPU resident.  A sequence of which one is not, or whose length does not fit its table,
+ * its weights or the destination, is left as it was in every array (its kept row is -1 throughout, its new length the old
+ * one), and the next call that checks the device status word returns PIE_ERR_NOT_RESIDENT / PIE_ERR_INVALID.
+ * With kept host copies every block of the layer counts as written.  Once all layers have evicted, the blocks behind the new
+ * length can be given back (pie_block_free).
+ * PIE_ERR_INVALID: budget < 1, recent < 0 or > budget, strides or widths that are not positive, a destination table
+ * that is the source's own array, weights_out == weights with another stride.  PIE_ERR_UNSUPPORTED while the compute stream is being captured. */
+int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, int32_t max_blocks_per_seq,
+                 const int32_t *ctx_lens_dev, int32_t n_seqs, float *weights, int64_t weights_stride, int32_t budget,
+                 int32_t recent, const int32_t *dst_block_table_dev, int32_t dst_max_blocks, float *weights_out,
+                 int64_t weights_out_stride, int32_t *new_lens_dev, int32_t *kept_dev);
+
 /* ---- kept host copies and write-back elision (a variant the paper does not have: Section 3.2 gives the
  * CPU region up once a unit has been swapped in) ---------------------------------------------------------
  * on != 0: a unit that is swapped in keeps its host slot; when it is swapped out again it returns to that slot, and

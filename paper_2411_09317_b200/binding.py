@@ -38,6 +38,7 @@ EXPORTS = [
     "pie_table_capacity", "pie_table_swap_ex", "pie_table_set_retention", "pie_table_kept_copies", "pie_table_mark_dirty", "pie_table_drop_host_copy", "pie_set_retention",
     "pie_declare_append_blocks", "pie_kv_write", "pie_prefill_attention", "pie_decode_layer", "pie_set_lookahead", "pie_set_run_ahead", "pie_set_kv_scales",
     "pie_governor_create", "pie_governor_destroy", "pie_governor_report", "pie_governor_state", "pie_report_throughput",
+    "pie_set_rope", "pie_rope_plan", "pie_rope_kv_write", "pie_prompt_attention", "pie_decode_attention_weights", "pie_kv_evict",
 ]
 
 
@@ -151,6 +152,12 @@ _sig = {
     "pie_controller_decide": (_f64, [_vp, _f64, _f64, _f64, _f64, _f64]),
     "pie_set_violation_trigger": (_i32, [_vp, _f64]),
     "pie_prefill_attention": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _f32]),
+    "pie_set_rope": (_i32, [_vp, _i32, _vp, _vp, _i32, _f32]),
+    "pie_rope_plan": (_i32, [_i32, _i32, _vp, _vp, _vp, ctypes.POINTER(_i32)]),
+    "pie_rope_kv_write": (_i32, [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i32, _i32, _i64, _i64, _i64]),
+    "pie_prompt_attention": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _f32, _i64, _i64, _i64]),
+    "pie_decode_attention_weights": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp, _i64]),
+    "pie_kv_evict": (_i32, [_vp, _i32, _vp, _i32, _vp, _i32, _vp, _i64, _i32, _i32, _vp, _i32, _vp, _i64, _vp, _vp]),
     "pie_fifo_counters": (_i32, [_vp, ctypes.POINTER(_i64), ctypes.POINTER(_i64)]),
     "pie_layer_controller_decide": (_i32, [_vp, _i32, _i32, _f64, _f64, _i64, _i64, _f64, _f64]),
     "pie_decode_attention_noalloc": (_i32, [_vp, _i64, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _i32,
@@ -220,6 +227,56 @@ def pie_prefill_attention(pool, layer, q, out, block_table_dev, max_blocks_per_s
     ch, qh = _np_i32(ctx_lens_host), _np_i32(q_offsets_host)
     check(lib.pie_prefill_attention(pool, layer, q, out, block_table_dev, max_blocks_per_seq, ctx_lens_dev, q_offsets_dev, _ptr(ch),
                                     _ptr(qh), n_seqs, scale), "pie_prefill_attention")
+
+
+def pie_set_rope(pool, rotary_dim, pair_axis, inv_freq, adjacent=0, amplitude=1.0) -> None:
+    """pair_axis (axis of each pair) and inv_freq (radians per position): host arrays of rotary_dim / 2 entries."""
+    axis, freq = _np_i32(pair_axis), np.ascontiguousarray(inv_freq, dtype=np.float64)
+    assert len(axis) == len(freq) == rotary_dim // 2
+    check(lib.pie_set_rope(pool, rotary_dim, _ptr(axis), _ptr(freq), int(adjacent), amplitude), "pie_set_rope")
+
+
+def pie_rope_plan(head_dim, rotary_dim, pair_axis, inv_freq):
+    """-> (2^64-ths of a turn per position, uint64 [rotary_dim / 2]; rows that positions must have)"""
+    axis, freq = _np_i32(pair_axis), np.ascontiguousarray(inv_freq, dtype=np.float64)
+    turns, n_axes = np.zeros(len(freq), np.uint64), _i32()
+    check(lib.pie_rope_plan(head_dim, rotary_dim, _ptr(axis), _ptr(freq), _ptr(turns), ctypes.byref(n_axes)), "pie_rope_plan")
+    return turns, n_axes.value
+
+
+def pie_rope_kv_write(pool, layer, q, q_out, k, k_out, v, positions_dev, token_seq_dev, token_pos_dev, n_tokens, block_table_dev,
+                      max_blocks_per_seq, n_seqs, q_stride=0, k_stride=0, v_stride=0) -> None:
+    """Device pointers (0 / None for NULL); strides in elements from a token to the next, 0 for dense rows."""
+    check(lib.pie_rope_kv_write(pool, layer, _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), _ptr(v), _ptr(positions_dev),
+                                _ptr(token_seq_dev), _ptr(token_pos_dev), n_tokens, _ptr(block_table_dev), max_blocks_per_seq, n_seqs,
+                                q_stride, k_stride, v_stride), "pie_rope_kv_write")
+
+
+def pie_prompt_attention(pool, q, k, v, out, offsets_host, n_seqs, scale, q_stride=0, k_stride=0, v_stride=0) -> None:
+    """q / k / v / out: device pointers; offsets_host [n_seqs + 1]: numpy int32; strides in elements, 0 for dense rows."""
+    off = _np_i32(offsets_host)
+    assert len(off) > n_seqs
+    check(lib.pie_prompt_attention(pool, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(off), n_seqs, scale, q_stride, k_stride, v_stride),
+          "pie_prompt_attention")
+
+
+def pie_decode_attention_weights(pool, layer, q, out, block_table_dev, max_blocks_per_seq, ctx_lens_dev, n_seqs, scale, weights,
+                                 weights_stride, block_table_host=None, ctx_lens_host=None, k_new=None, v_new=None) -> None:
+    """weights: device fp32 [n_seqs][n_kv_heads][weights_stride], added to."""
+    bth = None if block_table_host is None else _np_i32(block_table_host)
+    clh = None if ctx_lens_host is None else _np_i32(ctx_lens_host)
+    check(lib.pie_decode_attention_weights(pool, layer, _ptr(q), _ptr(out), _ptr(block_table_dev), max_blocks_per_seq, _ptr(ctx_lens_dev),
+                                           _ptr(bth), _ptr(clh), n_seqs, scale, _ptr(k_new), _ptr(v_new), _ptr(weights), weights_stride),
+          "pie_decode_attention_weights")
+
+
+def pie_kv_evict(pool, layer, block_table_dev, max_blocks_per_seq, ctx_lens_dev, n_seqs, weights, weights_stride, budget, recent,
+                 dst_block_table_dev=None, dst_max_blocks=0, weights_out=None, weights_out_stride=0, new_lens_dev=None,
+                 kept_dev=None) -> None:
+    """Device pointers; without dst_block_table_dev / weights_out the keys, values / weights are moved in place."""
+    check(lib.pie_kv_evict(pool, layer, _ptr(block_table_dev), max_blocks_per_seq, _ptr(ctx_lens_dev), n_seqs, _ptr(weights), weights_stride,
+                           budget, recent, _ptr(dst_block_table_dev), dst_max_blocks, _ptr(weights_out), weights_out_stride,
+                           _ptr(new_lens_dev), _ptr(kept_dev)), "pie_kv_evict")
 
 
 def pie_set_violation_trigger(pool, share) -> None:

@@ -485,6 +485,9 @@ struct AttnParams {
     float scale_log2e;      // softmax scale * log2(e) (* the key scale of an 8-bit pool)
     float out_scale = 1.f;  // 8-bit pools: the value scale (times what the kernel's 16-bit images of the bytes leave out)
     float k_scale = 1.f, v_scale = 1.f;  // 8-bit pools: the append stores E4M3(x / scale)
+    // Calls that accumulate attention weights (instantiations with SCORES): every valid token's scores, in log2 units, as
+    // [item][token of the chunk][head of the group] - see attn_weights_kernel.
+    float *scores = nullptr;
 };
 
 // KV8: the pool holds E4M3 bytes; a ring stage is then the 4 KiB byte tile as the TMA unit delivers it, and the consumer
@@ -681,7 +684,7 @@ __device__ __forceinline__ uint2 merge_piece(const float *__restrict__ part_o, i
 // CTAs per SM than shared memory lets in anyway (four of 50 KiB; without it some instantiations were capped at 96
 // registers and spilled).  The 8-bit kernel is bound by instruction latency, not by bytes in flight, and its CTAs need
 // less than half of the shared memory: five per SM (128 registers) measured 3-6 % faster than four.
-template <int D, bool BF16, int STAGES, int NW, bool KV8 = false>
+template <int D, bool BF16, int STAGES, int NW, bool KV8 = false, bool SCORES = false>
 __global__ void __launch_bounds__((NW + 1) * 32, KV8 ? 5 : 1)
 paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams p) {
     using SM = AttnSmem<D, STAGES, NW, KV8>;
@@ -1122,6 +1125,18 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             }
             float v0 = (sa[0] + sb[0]) * sl2e, v1 = (sa[1] + sb[1]) * sl2e;
             float v2 = (sa[2] + sb[2]) * sl2e, v3 = (sa[3] + sb[3]) * sl2e;
+            if constexpr (SCORES) {
+                // a tile's scores are one contiguous piece of 16 * group floats: the warp's four stores fill whole sectors
+                float *sc = p.scores + ((int64_t)item * p.split_tokens + 16 * i) * p.group;
+                if (c2 < p.group) {
+                    if (r0 < nvalid) sc[r0 * p.group + c2] = v0;
+                    if (r0 + 8 < nvalid) sc[(r0 + 8) * p.group + c2] = v2;
+                }
+                if (c2 + 1 < p.group) {
+                    if (r0 < nvalid) sc[r0 * p.group + c2 + 1] = v1;
+                    if (r0 + 8 < nvalid) sc[(r0 + 8) * p.group + c2 + 1] = v3;
+                }
+            }
             if (r0 >= nvalid) v0 = v1 = -INFINITY;
             if (r0 + 8 >= nvalid) v2 = v3 = -INFINITY;
             float x0 = fmaxf(v0, v2), x1 = fmaxf(v1, v3);
@@ -1259,6 +1274,10 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                 // the whole context in one chunk: normalise and round here
                 const float r = acc * (ll > 0.f ? 1.f / ll : 0.f);
                 p.out[out_row0 + e] = BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(r)) : __half_as_ushort(__float2half_rn(r));
+                if (SCORES && d == 0) {   // the weights need the maximum and the sum
+                    p.part_ml[((int64_t)item * p.group + g) * 2 + 0] = mm;
+                    p.part_ml[((int64_t)item * p.group + g) * 2 + 1] = ll;
+                }
             } else {
                 p.part_o[((int64_t)item * p.group + g) * D + d] = acc;
                 if (d == 0) {
@@ -1385,6 +1404,61 @@ combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_
         }
         const float r = acc * (ll > 0.f ? 1.f / ll : 0.f);
         out[row0 + g * D + d] = BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(r)) : __half_as_ushort(__float2half_rn(r));
+    }
+}
+
+// =====================================================================================================
+// Attention weights: the attention kernel has left every score (log2 units) and every chunk's maximum and sum per head;
+// a token's weight is the sum over its group's heads of 2^(score - m) / l, with m and l merged over the sequence's chunks.
+// Storing the scores costs 8 bytes per (token, query head), written and read once and mostly from L2; computing them again
+// from the keys would cost half of the cache's bytes a second time.  One CTA per item (chunk, KV head), items in turn.
+// =====================================================================================================
+constexpr int WEIGHTS_THREADS = 128;
+
+__global__ void __launch_bounds__(WEIGHTS_THREADS)
+attn_weights_kernel(const float *__restrict__ scores, const float *__restrict__ part_ml, const int32_t *__restrict__ chunk_off,
+                    const int32_t *__restrict__ ctx_lens, float *__restrict__ weights, int64_t stride, int32_t n_seqs, int32_t n_kv_heads,
+                    int32_t group, int32_t split_tokens, int32_t max_tokens, int32_t *status) {
+    __shared__ float sh_m[8], sh_inv[8];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int tid = threadIdx.x;
+    const int32_t n_items = chunk_off[n_seqs] * n_kv_heads;
+    for (int32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+        const int32_t ci = item / n_kv_heads, kvh = item - ci * n_kv_heads;
+        int32_t lo = 0, hi = n_seqs;  // largest s with chunk_off[s] <= ci
+        while (hi - lo > 1) {
+            const int32_t mid = (lo + hi) >> 1;
+            if (chunk_off[mid] <= ci) lo = mid;
+            else hi = mid;
+        }
+        const int32_t chunk0 = chunk_off[lo], nchunks = chunk_off[lo + 1] - chunk0;
+        const int32_t ctx = min(__ldg(ctx_lens + lo), max_tokens);
+        const int64_t t0 = (int64_t)(ci - chunk0) * split_tokens;
+        int32_t n = (int32_t)min((int64_t)split_tokens, ctx - t0);
+        if (t0 + n > stride) {   // no room for these tokens' weights
+            if (tid == 0) raise_status(status, STATUS_CTX_TOO_LONG);
+            n = (int32_t)max((int64_t)0, stride - t0);
+        }
+        if (tid < group) {   // merged over the chunks in chunk order
+            float mm = -INFINITY, ll = 0.f;
+            for (int32_t c = 0; c < nchunks; ++c) mm = fmaxf(mm, part_ml[((((int64_t)chunk0 + c) * n_kv_heads + kvh) * group + tid) * 2]);
+            for (int32_t c = 0; c < nchunks; ++c) {
+                const int64_t id = ((((int64_t)chunk0 + c) * n_kv_heads + kvh) * group + tid) * 2;
+                ll += part_ml[id + 1] * (part_ml[id] == -INFINITY ? 0.f : fast_exp2(part_ml[id] - mm));
+            }
+            sh_m[tid] = mm;
+            sh_inv[tid] = 1.f / ll;
+        }
+        __syncthreads();
+        float *wrow = weights + ((int64_t)lo * n_kv_heads + kvh) * stride + t0;
+        const float *sc = scores + (int64_t)item * split_tokens * group;
+        for (int32_t t = tid; t < n; t += WEIGHTS_THREADS) {
+            float w = 0.f;
+            for (int g = 0; g < group; ++g) w += fast_exp2(sc[(int64_t)t * group + g] - sh_m[g]) * sh_inv[g];
+            wrow[t] += w;
+        }
+        __syncthreads();
     }
 }
 
@@ -1520,6 +1594,29 @@ cudaError_t attn_configure(int head_dim, int dtype, int variant, int *ctas_per_s
     });
 }
 
+template <typename F>
+static cudaError_t dispatch_weights(int head_dim, int dtype, int kv_fp8, F &&f) {
+    // the default variants' shapes
+    if (kv_fp8)
+        return dtype == PIE_BF16 ? f(paged_decode_attn_kernel<128, true, 6, 2, true, true>, AttnSmem<128, 6, 2, true>::BYTES, 2)
+                                 : f(paged_decode_attn_kernel<128, false, 6, 2, true, true>, AttnSmem<128, 6, 2, true>::BYTES, 2);
+    if (head_dim == 128)
+        return dtype == PIE_BF16 ? f(paged_decode_attn_kernel<128, true, 4, 2, false, true>, AttnSmem<128, 4, 2>::BYTES, 2)
+                                 : f(paged_decode_attn_kernel<128, false, 4, 2, false, true>, AttnSmem<128, 4, 2>::BYTES, 2);
+    return dtype == PIE_BF16 ? f(paged_decode_attn_kernel<64, true, 4, 2, false, true>, AttnSmem<64, 4, 2>::BYTES, 2)
+                             : f(paged_decode_attn_kernel<64, false, 4, 2, false, true>, AttnSmem<64, 4, 2>::BYTES, 2);
+}
+
+cudaError_t attn_weights_configure(int head_dim, int dtype, int *ctas_per_sm, int kv_fp8) {
+    cudaError_t e0 = cudaFuncSetAttribute(attn_weights_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e0 != cudaSuccess) return e0;
+    return dispatch_weights(head_dim, dtype, kv_fp8, [&](auto kernel, int smem, int nw) -> cudaError_t {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        return cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, kernel, (nw + 1) * 32, smem);
+    });
+}
+
 int64_t attn_counter_words(int32_t, int32_t) { return 64; }  // [0] next item, [1] CTAs that have left
 
 cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const AttnLaunch &a, const CUtensorMap &map,
@@ -1581,6 +1678,28 @@ cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const A
         p.scale_log2e *= a.k_scale;  // scores over the stored keys are scores over the keys / k_scale
     }
     if (a.k_new == nullptr || a.v_new == nullptr) p.k_new = p.v_new = nullptr;
+    if (a.weights != nullptr) {
+        p.scores = sc.scores;
+        p.early_trigger = 0;
+        cudaError_t ew = dispatch_weights(sh.head_dim, sh.dtype, sh.kv_fp8, [&](auto kernel, int smem, int nw) -> cudaError_t {
+            kernel<<<a.grid, (nw + 1) * 32, smem, stream>>>(map, p);
+            return cudaGetLastError();
+        });
+        if (ew == cudaSuccess) ew = launch_combine(sh, sc, a.out, a.n_seqs, a.max_blocks, a.split_tokens, turn, stream);
+        if (ew != cudaSuccess) return ew;
+        cudaLaunchConfig_t lc = {};
+        lc.gridDim = dim3((unsigned)std::min<int64_t>(sc.max_items, 8 * (int64_t)a.grid));
+        lc.blockDim = dim3(WEIGHTS_THREADS);
+        lc.stream = stream;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        lc.attrs = at;
+        lc.numAttrs = 1;
+        return cudaLaunchKernelEx(&lc, attn_weights_kernel, (const float *)sc.scores, (const float *)p.part_ml, (const int32_t *)sc.chunk_off,
+                                  a.ctx_lens, a.weights, a.weights_stride, a.n_seqs, sh.n_kv_heads, (int32_t)p.group, a.split_tokens,
+                                  a.max_blocks * 16, a.status);
+    }
     cudaError_t e = dispatch_variant(sh.head_dim, sh.dtype, a.variant, sh.kv_fp8, [&](auto kernel, int smem, int nw) -> cudaError_t {
         if (!a.dependent_launch) {
             kernel<<<a.grid, (nw + 1) * 32, smem, stream>>>(map, p);

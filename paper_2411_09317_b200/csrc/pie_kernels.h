@@ -42,6 +42,8 @@ cudaError_t launch_kv_write8(const void *k, const void *v, const int32_t *token_
                              float k_scale, float v_scale, int32_t *status, cudaStream_t stream);
 
 // ---- attention -----------------------------------------------------------------------------------
+constexpr int ROPE_PAIRS = 64;  // head_dim / 2 at most
+
 struct AttnShape {
     int head_dim;      // 64 or 128
     int dtype;         // PIE_F16 / PIE_BF16
@@ -50,6 +52,59 @@ struct AttnShape {
     int64_t n_gpu_slots;
     int kv_fp8 = 0;    // blocks hold E4M3 bytes (head_dim 128 only)
 };
+
+// ---- rotary positions, fused with the cache write ---------------------------------------------------
+struct RopeTable {
+    uint64_t turns[ROPE_PAIRS];  // 2^64-ths of a turn per position
+    uint8_t axis[ROPE_PAIRS];    // which row of the positions turns the pair
+    int32_t rotary_dim = 0;      // 0: not set
+    int32_t n_axes = 0;
+    int32_t adjacent = 0;        // pair i: elements (2i, 2i + 1) instead of (i, i + rotary_dim / 2)
+    float amplitude = 1.f;
+};
+struct RopeLaunch {
+    const void *q, *k, *v;       // q or k may be NULL; strides in elements
+    void *q_out, *k_out;         // k_out may be NULL
+    const int32_t *positions;    // device [n_axes][n_tokens]
+    const int32_t *token_seq, *token_pos, *block_table;  // block_table NULL: no cache write
+    const int32_t *slot_table;
+    void *gpu_pool;
+    int64_t n_tokens, q_stride, k_stride, v_stride;
+    int32_t max_blocks, n_seqs;
+    float k_scale, v_scale;
+    int32_t *status;
+};
+cudaError_t rope_configure();
+cudaError_t launch_rope_kv(const AttnShape &sh, const RopeLaunch &a, const RopeTable &table, int n_sms, cudaStream_t stream);
+
+// ---- attention over whole prompts ---------------------------------------------------------------------
+struct PromptLaunch {
+    const void *q, *k, *v;      // strides in elements
+    void *out;
+    const int32_t *offsets;     // device [n_seqs + 1]
+    int64_t q_stride, k_stride, v_stride, n_tokens;
+    int32_t n_seqs;
+    float scale;
+    int32_t *status;
+};
+cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, cudaStream_t stream);
+
+// ---- eviction by accumulated attention weight ------------------------------------------------------------
+struct EvictLaunch {
+    const int32_t *block_table, *ctx_lens, *dst_table;   // dst_table NULL: in place
+    const int32_t *slot_table;
+    const float *weights;
+    float *weights_out;
+    int64_t weights_stride, weights_out_stride;
+    int32_t *new_lens, *kept;    // may be NULL
+    int32_t *rows;               // scratch [n_seqs * n_kv_heads][budget]: slot * 16 + row of each kept token
+    int32_t *counts;             // scratch [n_seqs * n_kv_heads]: kept tokens, -1: the sequence is left alone
+    void *gpu_pool;
+    int32_t max_blocks, dst_max_blocks, n_seqs, budget, recent;
+    int32_t *status;
+};
+cudaError_t evict_configure();
+cudaError_t launch_evict(const AttnShape &sh, const EvictLaunch &a, int n_sms, cudaStream_t stream);
 
 struct AttnScratch {
     int32_t *chunk_off;  // [max_seqs + 1] (used only for batches beyond the in-kernel plan)
@@ -60,6 +115,7 @@ struct AttnScratch {
     float *part_ml_more[2] = {nullptr, nullptr};  // AttnLaunch::defer_combine; the counters then hold three sets of four words)
     int64_t max_items;   // capacity in items (chunk, kv head)
     int32_t max_seqs;
+    float *scores = nullptr;  // [max_items][split_tokens][G] (calls that accumulate weights; allocated at the first of them)
 };
 
 struct AttnLaunch {
@@ -98,6 +154,10 @@ struct AttnLaunch {
     bool defer_combine = false;
     void *prev_out = nullptr;
     int parity = 0;
+    // Accumulated attention weights: device fp32 [n_seqs][n_kv_heads][weights_stride], or NULL.  The kernel then leaves every
+    // score in the scratch, and one more kernel turns them into weights (variant 0 only; not deferred).
+    float *weights = nullptr;
+    int64_t weights_stride = 0;
 };
 
 // Build the TMA descriptors of the HBM pool: map3d covers a whole K+V tile in one copy
@@ -108,6 +168,7 @@ cudaError_t make_pool_tensor_maps(void *gpu_pool, int64_t n_gpu_slots, int n_kv_
 int attn_smem_bytes(int head_dim);
 int64_t attn_counter_words(int32_t max_seqs, int32_t n_kv_heads);
 cudaError_t attn_configure(int head_dim, int dtype, int variant, int *ctas_per_sm, int kv_fp8 = 0);
+cudaError_t attn_weights_configure(int head_dim, int dtype, int *ctas_per_sm, int kv_fp8);
 cudaError_t make_pool_tensor_map_fp8(void *gpu_pool, int64_t n_gpu_slots, int n_kv_heads, CUtensorMap *map2d);
 cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const AttnLaunch &a, const CUtensorMap &map,
                              int use3d, cudaStream_t stream);

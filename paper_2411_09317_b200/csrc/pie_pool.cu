@@ -134,6 +134,12 @@ struct pie_pool {
     CUtensorMap map3d{}, map2d{};
     CUtensorMap map_prefill{};   // the pool's K and V rows as 16-row tiles (chunked-prefill attention; 16-bit pools)
     bool prefill_ready = false;
+    bool rope_ready = false, evict_ready = false;
+    pie::RopeTable rope{};       // rotary_dim 0: not set (pie_set_rope)
+    int attn_weights_grid = 0;   // 0: not configured yet
+    int32_t *evict_scratch = nullptr;   // per kept token its row, per (sequence, KV head) the number of them
+    int64_t evict_words = 0;
+    int device = 0;
     int use3d = 0, attn_grid = 0, n_sms = 0;
     // decode-step staging (device copies of host inputs)
     void *stage_q = nullptr, *stage_out = nullptr, *stage_k = nullptr, *stage_v = nullptr;
@@ -799,6 +805,8 @@ void destroy_pool(pie_pool *p) {
     cudaFree(p->scratch.counters);
     cudaFree(p->scratch.part_o);
     cudaFree(p->scratch.part_ml);
+    cudaFree(p->scratch.scores);
+    cudaFree(p->evict_scratch);
     for (int t = 0; t < 2; ++t) {
         cudaFree(p->scratch.part_o_more[t]);
         cudaFree(p->scratch.part_ml_more[t]);
@@ -836,7 +844,8 @@ int flush_deferred_combine(pie_pool *p) {
 // flush_deferred_combine); a merge that an earlier call left (p->deferred) is taken on by this call's kernel.
 int attention_call(pie_pool *p, int32_t layer, const void *q, void *out, const int32_t *bt_dev, int32_t max_blocks,
                    const int32_t *ctx_dev, const int32_t *bt_host, const int32_t *ctx_host, int32_t n_seqs, float scale,
-                   const void *k_new, const void *v_new, bool dependent = false, bool defer = false, bool in_loop = false) {
+                   const void *k_new, const void *v_new, bool dependent = false, bool defer = false, bool in_loop = false,
+                   float *weights = nullptr, int64_t weights_stride = 0) {
     if (!p) return PIE_ERR_INVALID;
     if (p->sticky != PIE_OK) return p->sticky;
     if (layer < 0 || layer >= p->cfg.n_layers) return PIE_ERR_RANGE;
@@ -871,6 +880,7 @@ int attention_call(pie_pool *p, int32_t layer, const void *q, void *out, const i
         for (int32_t s = 0; s < n_seqs; ++s) {
             const int32_t ctx = ctx_host[s];
             if (ctx < 0 || ctx > max_blocks * 16) return PIE_ERR_INVALID;
+            if (weights && ctx > weights_stride) return PIE_ERR_INVALID;
             chunks += (ctx + split - 1) / split;
             for (int32_t b = 0; b < (ctx + 15) / 16; ++b) p->v_in.push_back(bt_host[(int64_t)s * max_blocks + b]);
         }
@@ -942,6 +952,11 @@ int attention_call(pie_pool *p, int32_t layer, const void *q, void *out, const i
     a.done_word = p->done_dev;
     a.done_value = (unsigned long long)ticket;
     a.dependent_launch = dependent;
+    if (weights) {
+        a.grid = p->attn_weights_grid;
+        a.weights = weights;
+        a.weights_stride = weights_stride;
+    }
     // a merge the call before this one left: this kernel takes it on if it attends the same batch (else it is merged now)
     if (p->deferred.on && !(dependent && p->deferred.n_seqs == n_seqs && p->deferred.max_blocks == max_blocks && p->deferred.ctx == ctx_dev &&
                             p->deferred.split == (int32_t)split)) {
@@ -1187,6 +1202,71 @@ int finish_group(pie_pool *p) {
     return st != PIE_OK ? st : st2;
 }
 
+// ---- helpers of the calls that go beside the attention (rotary write, whole prompts, eviction)
+// the calling thread's current device is the pool's while this lives
+struct OnDevice {
+    int was = -1;
+    explicit OnDevice(int dev) {
+        if (cudaGetDevice(&was) != cudaSuccess || was == dev || cudaSetDevice(dev) != cudaSuccess) was = -1;
+    }
+    ~OnDevice() {
+        if (was >= 0) cudaSetDevice(was);
+    }
+};
+
+// n rows of `row` 16-bit elements, `stride` elements apart
+struct Rows {
+    const void *p;
+    int64_t n, row, stride;
+    bool aligned() const { return !p || (((uintptr_t)p & 15) == 0 && stride % 8 == 0 && stride >= row); }
+    bool overlaps(const Rows &o) const {
+        if (!p || !o.p || n <= 0 || o.n <= 0) return false;
+        const uintptr_t a = (uintptr_t)p, b = (uintptr_t)o.p;
+        return a < b + (uintptr_t)((o.n - 1) * o.stride + o.row) * 2 && b < a + (uintptr_t)((n - 1) * stride + row) * 2;
+    }
+};
+
+// is the compute stream being captured into a graph?  (A replay would pass the host's books by.)
+bool capturing(pie_pool *p) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(p->stream[PIE_Q_COMPUTE], &status) != cudaSuccess) {
+        cudaGetLastError();
+        return true;
+    }
+    return status != cudaStreamCaptureStatusNone;
+}
+
+pie::AttnShape pool_shape(const pie_pool *p) {
+    return pie::AttnShape{p->cfg.head_dim, p->cfg.dtype, p->cfg.n_q_heads, p->cfg.n_kv_heads, p->cfg.n_logical_blocks,
+                          p->cfg.n_gpu_slots, p->kv_fp8};
+}
+
+// Work on a layer's units on the compute stream, like an attention call: a compute ticket, behind every copy that is still
+// bringing a unit of the layer in; what is swapped out afterwards waits for it.
+int begin_layer_work(pie_pool *p, int32_t layer, bool writes, int64_t *ticket) {
+    int64_t waits[4];
+    int st = p->table->attention(layer, nullptr, 0, ticket, waits);
+    if (st != PIE_OK) return st;
+    if (writes && p->table->tracks_writes()) p->table->mark_layer_dirty(layer);  // which blocks are written is on the device only
+    st = reserve_ticket_event(p, PIE_Q_COMPUTE, *ticket);
+    for (int qd = 1; qd <= 2 && st == PIE_OK; ++qd) st = wait_ticket(p, p->stream[PIE_Q_COMPUTE], qd, waits[qd]);
+    if (st != PIE_OK) p->sticky = st;
+    return st;
+}
+
+// ticket 0: work that touches no unit
+int end_layer_work(pie_pool *p, cudaError_t e, int64_t ticket) {
+    if (e != cudaSuccess) {
+        g_last_cuda_error = (int)e;
+        p->sticky = PIE_ERR_CUDA;
+        return PIE_ERR_CUDA;
+    }
+    if (ticket == 0) return PIE_OK;
+    const int st = record_ticket(p, PIE_Q_COMPUTE, ticket);
+    if (st != PIE_OK) p->sticky = st;
+    return st;
+}
+
 // streams and the arrival word of the host-buffer entry point's pipeline (created at its first use)
 int ensure_io(pie_pool *p) {
     if (p->io_stream[0]) return PIE_OK;
@@ -1303,6 +1383,7 @@ int pie_pool_create(const pie_pool_config *cfg_in, pie_pool **out) {
     p->kv_fp8 = cfg->kv_format;
     p->block_bytes = (int64_t)2 * 16 * cfg->n_kv_heads * cfg->head_dim * (p->kv_fp8 ? 1 : 2);
     p->n_sms = prop.multiProcessorCount;
+    p->device = dev;
     p->table = new (std::nothrow) pie::Table(cfg->n_layers, cfg->n_logical_blocks, cfg->n_gpu_slots, cfg->n_host_slots);
     if (!p->table) { destroy_pool(p); return PIE_ERR_NOMEM; }
     if (cfg->visible_blocks != 0 && p->table->init_capacity(cfg->visible_blocks) != PIE_OK) { destroy_pool(p); return PIE_ERR_INVALID; }
@@ -1993,6 +2074,245 @@ int pie_prefill_attention(pie_pool *pool, int32_t layer, const void *q, void *ou
     if (st == PIE_OK) st = record_ticket(pool, PIE_Q_COMPUTE, ticket);
     if (st != PIE_OK) pool->sticky = st;
     return st;
+}
+
+// ---- rotary positions, whole prompts, attention weights, eviction ---------------------------------------------------
+
+int pie_set_rope(pie_pool *pool, int32_t rotary_dim, const int32_t *pair_axis, const double *inv_freq, int32_t adjacent,
+                 float amplitude) {
+    if (!pool || !std::isfinite(amplitude) || !(amplitude > 0.f)) return PIE_ERR_INVALID;
+    pie::RopeTable t;
+    int st = pie_rope_plan(pool->cfg.head_dim, rotary_dim, pair_axis, inv_freq, t.turns, &t.n_axes);
+    if (st != PIE_OK) return st;
+    for (int32_t i = 0; i < rotary_dim / 2; ++i) t.axis[i] = (uint8_t)pair_axis[i];
+    t.rotary_dim = rotary_dim;
+    t.adjacent = adjacent != 0;
+    t.amplitude = amplitude;
+    pool->rope = t;
+    return PIE_OK;
+}
+
+int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out, const void *k, void *k_out, const void *v,
+                      const int32_t *positions_dev, const int32_t *token_seq_dev, const int32_t *token_pos_dev,
+                      int64_t n_tokens, const int32_t *block_table_dev, int32_t max_blocks_per_seq, int32_t n_seqs,
+                      int64_t q_stride, int64_t k_stride, int64_t v_stride) {
+    if (!pool || n_tokens < 0) return PIE_ERR_INVALID;
+    if (pool->sticky != PIE_OK) return pool->sticky;
+    if (layer < 0 || layer >= pool->cfg.n_layers) return PIE_ERR_RANGE;
+    if (pool->rope.rotary_dim == 0) return PIE_ERR_INVALID;
+    const bool write = block_table_dev != nullptr;
+    const int64_t D = pool->cfg.head_dim, q_row = pool->cfg.n_q_heads * D, kv_row = pool->cfg.n_kv_heads * D;
+    if (q_stride == 0) q_stride = q_row;
+    if (k_stride == 0) k_stride = kv_row;
+    if (v_stride == 0) v_stride = kv_row;
+    if (write && (max_blocks_per_seq <= 0 || n_seqs <= 0)) return PIE_ERR_INVALID;
+    if (n_tokens > 0) {
+        if (!positions_dev || (!q && !k) || (q != nullptr) != (q_out != nullptr) || (!k && k_out)) return PIE_ERR_INVALID;
+        if (write && (!k || !v || !token_seq_dev || !token_pos_dev)) return PIE_ERR_INVALID;
+        if (!write && k && !k_out) return PIE_ERR_INVALID;
+        const Rows in_q{q, n_tokens, q_row, q_stride}, in_k{k, n_tokens, kv_row, k_stride}, in_v{write ? v : nullptr, n_tokens, kv_row, v_stride};
+        const Rows out_q{q_out, n_tokens, q_row, q_row}, out_k{k_out, n_tokens, kv_row, kv_row};
+        for (const Rows &r : {in_q, in_k, in_v, out_q, out_k})
+            if (!r.aligned()) return PIE_ERR_INVALID;
+        // an output may be its own (dense) input; otherwise it overlaps nothing
+        if (out_q.overlaps(in_k) || out_q.overlaps(in_v) || out_q.overlaps(out_k) || out_k.overlaps(in_q) || out_k.overlaps(in_v)) return PIE_ERR_INVALID;
+        if (out_q.overlaps(in_q) && !(q == q_out && q_stride == q_row)) return PIE_ERR_INVALID;
+        if (out_k.overlaps(in_k) && !(k == k_out && k_stride == kv_row)) return PIE_ERR_INVALID;
+    }
+    OnDevice on(pool->device);
+    if (capturing(pool)) return PIE_ERR_UNSUPPORTED;
+    int st = poll(pool);
+    if (st != PIE_OK) return st;
+    st = check_status_word(pool);
+    if (st != PIE_OK) return st;
+    if (n_tokens == 0) return PIE_OK;
+    if (!pool->rope_ready) {
+        PIE_CUDA(pie::rope_configure());
+        pool->rope_ready = true;
+    }
+    cudaStream_t stream = pool->stream[PIE_Q_COMPUTE];
+    int64_t ticket = 0;
+    if (write) {
+        st = begin_layer_work(pool, layer, true, &ticket);
+        if (st != PIE_OK) return st;
+    }
+    pie::RopeLaunch a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.positions = positions_dev;
+    a.token_seq = token_seq_dev;
+    a.token_pos = token_pos_dev;
+    a.block_table = block_table_dev;
+    a.slot_table = pool->slot_table_dev + (int64_t)layer * pool->cfg.n_logical_blocks;
+    a.gpu_pool = pool->gpu_base;
+    a.n_tokens = n_tokens;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.max_blocks = max_blocks_per_seq;
+    a.n_seqs = n_seqs;
+    a.k_scale = pool->k_scale;
+    a.v_scale = pool->v_scale;
+    a.status = pool->status_dev;
+    return end_layer_work(pool, pie::launch_rope_kv(pool_shape(pool), a, pool->rope, pool->n_sms, stream), ticket);
+}
+
+int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const void *v, void *out, const int32_t *offsets_host,
+                         int32_t n_seqs, float scale, int64_t q_stride, int64_t k_stride, int64_t v_stride) {
+    if (!pool || n_seqs < 0) return PIE_ERR_INVALID;
+    if (pool->sticky != PIE_OK) return pool->sticky;
+    if (n_seqs > 0) {
+        if (!offsets_host || offsets_host[0] != 0) return PIE_ERR_INVALID;
+        for (int32_t s = 0; s < n_seqs; ++s)
+            if (offsets_host[s + 1] < offsets_host[s]) return PIE_ERR_INVALID;
+    }
+    const int64_t n_tokens = n_seqs > 0 ? offsets_host[n_seqs] : 0;
+    const int64_t D = pool->cfg.head_dim, q_row = pool->cfg.n_q_heads * D, kv_row = pool->cfg.n_kv_heads * D;
+    if (q_stride == 0) q_stride = q_row;
+    if (k_stride == 0) k_stride = kv_row;
+    if (v_stride == 0) v_stride = kv_row;
+    if (n_tokens > 0) {
+        if (!q || !k || !v || !out) return PIE_ERR_INVALID;
+        const Rows in_q{q, n_tokens, q_row, q_stride}, in_k{k, n_tokens, kv_row, k_stride}, in_v{v, n_tokens, kv_row, v_stride};
+        const Rows o{out, n_tokens, q_row, q_row};
+        for (const Rows &r : {in_q, in_k, in_v, o})
+            if (!r.aligned()) return PIE_ERR_INVALID;
+        if (o.overlaps(in_q) || o.overlaps(in_k) || o.overlaps(in_v)) return PIE_ERR_INVALID;
+    }
+    OnDevice on(pool->device);
+    if (capturing(pool)) return PIE_ERR_UNSUPPORTED;
+    int st = poll(pool);
+    if (st != PIE_OK) return st;
+    st = check_status_word(pool);
+    if (st != PIE_OK) return st;
+    if (n_tokens == 0) return PIE_OK;
+    cudaStream_t stream = pool->stream[PIE_Q_COMPUTE];
+    int64_t off = 0;
+    st = list_alloc(pool, n_seqs + 1, &off);
+    if (st != PIE_OK) return st;
+    std::memcpy(pool->list_host + off, offsets_host, (size_t)(n_seqs + 1) * 4);
+    cudaError_t e = cudaMemcpyAsync(pool->list_dev + off, pool->list_host + off, (size_t)(n_seqs + 1) * 4, cudaMemcpyHostToDevice, stream);
+    if (e == cudaSuccess) {
+        pie::PromptLaunch a{};
+        a.q = q;
+        a.k = k;
+        a.v = v;
+        a.out = out;
+        a.offsets = pool->list_dev + off;
+        a.q_stride = q_stride;
+        a.k_stride = k_stride;
+        a.v_stride = v_stride;
+        a.n_tokens = n_tokens;
+        a.n_seqs = n_seqs;
+        a.scale = scale;
+        a.status = pool->status_dev;
+        e = pie::launch_prompt_attention(pool_shape(pool), a, stream);
+    }
+    st = end_layer_work(pool, e, 0);
+    if (st == PIE_OK) {
+        st = list_commit(pool, off, n_seqs + 1, stream);
+        if (st != PIE_OK) pool->sticky = st;
+    }
+    return st;
+}
+
+int pie_decode_attention_weights(pie_pool *pool, int32_t layer, const void *q, void *out, const int32_t *block_table_dev,
+                                 int32_t max_blocks_per_seq, const int32_t *ctx_lens_dev, const int32_t *block_table_host,
+                                 const int32_t *ctx_lens_host, int32_t n_seqs, float scale, const void *k_new,
+                                 const void *v_new, float *weights, int64_t weights_stride) {
+    if (!pool || !weights || weights_stride <= 0 || ((uintptr_t)weights & 3)) return PIE_ERR_INVALID;
+    if (pool->sticky != PIE_OK) return pool->sticky;
+    OnDevice on(pool->device);
+    if (capturing(pool)) return PIE_ERR_UNSUPPORTED;
+    if (pool->attn_weights_grid == 0) {
+        int per_sm = 0;
+        PIE_CUDA(pie::attn_weights_configure(pool->cfg.head_dim, pool->cfg.dtype, &per_sm, pool->kv_fp8));
+        if (per_sm <= 0) return PIE_ERR_UNSUPPORTED;
+        if (pool->cfg.attn_ctas_per_sm > 0) per_sm = std::min(per_sm, pool->cfg.attn_ctas_per_sm);
+        const size_t bytes = (size_t)pool->scratch.max_items * (size_t)pool->cfg.split_tokens * (size_t)(pool->cfg.n_q_heads / pool->cfg.n_kv_heads) * 4;
+        const cudaError_t e = cudaMalloc((void **)&pool->scratch.scores, bytes);
+        if (e != cudaSuccess) {
+            cudaGetLastError();   // (an allocation that failed leaves the device as it was)
+            pool->scratch.scores = nullptr;
+            g_last_cuda_error = (int)e;
+            return PIE_ERR_NOMEM;
+        }
+        pool->attn_weights_grid = per_sm * pool->n_sms;
+    }
+    return attention_call(pool, layer, q, out, block_table_dev, max_blocks_per_seq, ctx_lens_dev, block_table_host, ctx_lens_host,
+                          n_seqs, scale, k_new, v_new, false, false, false, weights, weights_stride);
+}
+
+int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, int32_t max_blocks_per_seq,
+                 const int32_t *ctx_lens_dev, int32_t n_seqs, float *weights, int64_t weights_stride, int32_t budget,
+                 int32_t recent, const int32_t *dst_block_table_dev, int32_t dst_max_blocks, float *weights_out,
+                 int64_t weights_out_stride, int32_t *new_lens_dev, int32_t *kept_dev) {
+    if (!pool || n_seqs < 0 || max_blocks_per_seq <= 0 || budget < 1 || recent < 0 || recent > budget) return PIE_ERR_INVALID;
+    if (pool->sticky != PIE_OK) return pool->sticky;
+    if (layer < 0 || layer >= pool->cfg.n_layers) return PIE_ERR_RANGE;
+    if (n_seqs > 0 && (!block_table_dev || !ctx_lens_dev || !weights || weights_stride <= 0)) return PIE_ERR_INVALID;
+    if (dst_block_table_dev && (dst_max_blocks <= 0 || dst_block_table_dev == block_table_dev)) return PIE_ERR_INVALID;
+    if (!weights_out) {
+        weights_out = weights;
+        weights_out_stride = weights_stride;
+    } else if (weights_out_stride <= 0 || (weights_out == weights && weights_out_stride != weights_stride)) {
+        return PIE_ERR_INVALID;
+    }
+    const int64_t pairs = (int64_t)n_seqs * pool->cfg.n_kv_heads;
+    if (pairs > 0x7fffffffll) return PIE_ERR_INVALID;
+    OnDevice on(pool->device);
+    if (capturing(pool)) return PIE_ERR_UNSUPPORTED;
+    int st = poll(pool);
+    if (st != PIE_OK) return st;
+    st = check_status_word(pool);
+    if (st != PIE_OK) return st;
+    if (n_seqs == 0) return PIE_OK;
+    if (!pool->evict_ready) {
+        PIE_CUDA(pie::evict_configure());
+        pool->evict_ready = true;
+    }
+    // scratch: the kept tokens' rows and the counts; grows when a call needs more (cudaFree waits for the calls before it)
+    const int64_t words = pairs * ((int64_t)budget + 1);
+    if (words > pool->evict_words) {
+        cudaFree(pool->evict_scratch);
+        pool->evict_scratch = nullptr;
+        pool->evict_words = 0;
+        const cudaError_t e = cudaMalloc((void **)&pool->evict_scratch, (size_t)words * 4);
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            pool->evict_scratch = nullptr;
+            g_last_cuda_error = (int)e;
+            return PIE_ERR_NOMEM;
+        }
+        pool->evict_words = words;
+    }
+    int64_t ticket = 0;
+    st = begin_layer_work(pool, layer, true, &ticket);
+    if (st != PIE_OK) return st;
+    pie::EvictLaunch a{};
+    a.block_table = block_table_dev;
+    a.ctx_lens = ctx_lens_dev;
+    a.dst_table = dst_block_table_dev;
+    a.slot_table = pool->slot_table_dev + (int64_t)layer * pool->cfg.n_logical_blocks;
+    a.weights = weights;
+    a.weights_out = weights_out;
+    a.weights_stride = weights_stride;
+    a.weights_out_stride = weights_out_stride;
+    a.new_lens = new_lens_dev;
+    a.kept = kept_dev;
+    a.counts = pool->evict_scratch;
+    a.rows = pool->evict_scratch + pairs;
+    a.gpu_pool = pool->gpu_base;
+    a.max_blocks = max_blocks_per_seq;
+    a.dst_max_blocks = dst_max_blocks;
+    a.n_seqs = n_seqs;
+    a.budget = budget;
+    a.recent = recent;
+    a.status = pool->status_dev;
+    return end_layer_work(pool, pie::launch_evict(pool_shape(pool), a, pool->n_sms, pool->stream[PIE_Q_COMPUTE]), ticket);
 }
 
 int pie_report_throughput(pie_pool *pool, double throughput) {
