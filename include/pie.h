@@ -405,6 +405,13 @@ int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out,
  * being captured. */
 int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const void *v, void *out, const int32_t *offsets_host,
                          int32_t n_seqs, float scale, int64_t q_stride, int64_t k_stride, int64_t v_stride);
+/* The host half of pie_prompt_attention by itself (needs no GPU): checks the offsets and cuts the sequences into items of
+ * item_tokens consecutive tokens (the last of a sequence may have fewer), the ones that see the most keys first.
+ * items (host, capacity quadruples of int32, or NULL to ask for the count only): {the sequence's first token, the item's first
+ * token within the sequence, the sequence's length, the sequence}.  *n_items: their number.
+ * PIE_ERR_NOMEM: more items than capacity. */
+int pie_prompt_plan(const int32_t *offsets, int32_t n_seqs, int32_t item_tokens, int32_t *items, int64_t capacity,
+                    int64_t *n_items);
 
 /* ---- attention weights and eviction ------------------------------------------------------------------------------
  * (No counterpart in the paper: a cache that forgets costs neither HBM nor link.)

@@ -38,7 +38,7 @@ EXPORTS = [
     "pie_table_capacity", "pie_table_swap_ex", "pie_table_set_retention", "pie_table_kept_copies", "pie_table_mark_dirty", "pie_table_drop_host_copy", "pie_set_retention",
     "pie_declare_append_blocks", "pie_kv_write", "pie_prefill_attention", "pie_decode_layer", "pie_set_lookahead", "pie_set_run_ahead", "pie_set_kv_scales",
     "pie_governor_create", "pie_governor_destroy", "pie_governor_report", "pie_governor_state", "pie_report_throughput",
-    "pie_set_rope", "pie_rope_plan", "pie_rope_kv_write", "pie_prompt_attention", "pie_decode_attention_weights", "pie_kv_evict",
+    "pie_set_rope", "pie_rope_plan", "pie_rope_kv_write", "pie_prompt_attention", "pie_prompt_plan", "pie_decode_attention_weights", "pie_kv_evict",
 ]
 
 
@@ -156,6 +156,7 @@ _sig = {
     "pie_rope_plan": (_i32, [_i32, _i32, _vp, _vp, _vp, ctypes.POINTER(_i32)]),
     "pie_rope_kv_write": (_i32, [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i32, _i32, _i64, _i64, _i64]),
     "pie_prompt_attention": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _f32, _i64, _i64, _i64]),
+    "pie_prompt_plan": (_i32, [_vp, _i32, _i32, _vp, _i64, ctypes.POINTER(_i64)]),
     "pie_decode_attention_weights": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _f32, _vp, _vp, _vp, _i64]),
     "pie_kv_evict": (_i32, [_vp, _i32, _vp, _i32, _vp, _i32, _vp, _i64, _i32, _i32, _vp, _i32, _vp, _i64, _vp, _vp]),
     "pie_fifo_counters": (_i32, [_vp, ctypes.POINTER(_i64), ctypes.POINTER(_i64)]),
@@ -258,6 +259,15 @@ def pie_prompt_attention(pool, q, k, v, out, offsets_host, n_seqs, scale, q_stri
     assert len(off) > n_seqs
     check(lib.pie_prompt_attention(pool, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(off), n_seqs, scale, q_stride, k_stride, v_stride),
           "pie_prompt_attention")
+
+
+def pie_prompt_plan(offsets, item_tokens) -> np.ndarray:
+    """-> items int32 [n][4]: first token of the sequence, first token of the item within it, the sequence's length, the sequence"""
+    off, n = _np_i32(offsets), _i64()
+    check(lib.pie_prompt_plan(_ptr(off), len(off) - 1, item_tokens, None, 0, ctypes.byref(n)), "pie_prompt_plan")
+    items = np.zeros((max(n.value, 1), 4), np.int32)
+    check(lib.pie_prompt_plan(_ptr(off), len(off) - 1, item_tokens, _ptr(items), n.value, ctypes.byref(n)), "pie_prompt_plan")
+    return items[:n.value]
 
 
 def pie_decode_attention_weights(pool, layer, q, out, block_table_dev, max_blocks_per_seq, ctx_lens_dev, n_seqs, scale, weights,

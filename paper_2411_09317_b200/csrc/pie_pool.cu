@@ -134,7 +134,7 @@ struct pie_pool {
     CUtensorMap map3d{}, map2d{};
     CUtensorMap map_prefill{};   // the pool's K and V rows as 16-row tiles (chunked-prefill attention; 16-bit pools)
     bool prefill_ready = false;
-    bool rope_ready = false, evict_ready = false;
+    bool rope_ready = false, prompt_ready = false, evict_ready = false;
     pie::RopeTable rope{};       // rotary_dim 0: not set (pie_set_rope)
     int attn_weights_grid = 0;   // 0: not configured yet
     int32_t *evict_scratch = nullptr;   // per kept token its row, per (sequence, KV head) the number of them
@@ -2164,11 +2164,11 @@ int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const voi
                          int32_t n_seqs, float scale, int64_t q_stride, int64_t k_stride, int64_t v_stride) {
     if (!pool || n_seqs < 0) return PIE_ERR_INVALID;
     if (pool->sticky != PIE_OK) return pool->sticky;
-    if (n_seqs > 0) {
-        if (!offsets_host || offsets_host[0] != 0) return PIE_ERR_INVALID;
-        for (int32_t s = 0; s < n_seqs; ++s)
-            if (offsets_host[s + 1] < offsets_host[s]) return PIE_ERR_INVALID;
-    }
+    const int32_t tile_tokens = 128 / (pool->cfg.n_q_heads / pool->cfg.n_kv_heads);   // two tiles of 128 rows per item
+    int64_t n_items = 0;
+    int st = pie_prompt_plan(offsets_host, n_seqs, 2 * tile_tokens, nullptr, 0, &n_items);
+    if (st != PIE_OK) return st;
+    if (n_items * pool->cfg.n_kv_heads > 0x7fffffffll || n_items * 4 > pool->list_words / 2) return PIE_ERR_INVALID;
     const int64_t n_tokens = n_seqs > 0 ? offsets_host[n_seqs] : 0;
     const int64_t D = pool->cfg.head_dim, q_row = pool->cfg.n_q_heads * D, kv_row = pool->cfg.n_kv_heads * D;
     if (q_stride == 0) q_stride = q_row;
@@ -2184,36 +2184,42 @@ int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const voi
     }
     OnDevice on(pool->device);
     if (capturing(pool)) return PIE_ERR_UNSUPPORTED;
-    int st = poll(pool);
+    st = poll(pool);
     if (st != PIE_OK) return st;
     st = check_status_word(pool);
     if (st != PIE_OK) return st;
     if (n_tokens == 0) return PIE_OK;
+    if (!pool->prompt_ready) {
+        PIE_CUDA(pie::prompt_configure(pool->cfg.head_dim, pool->cfg.dtype));
+        pool->prompt_ready = true;
+    }
     cudaStream_t stream = pool->stream[PIE_Q_COMPUTE];
     int64_t off = 0;
-    st = list_alloc(pool, n_seqs + 1, &off);
+    st = list_alloc(pool, 4 * n_items, &off);
     if (st != PIE_OK) return st;
-    std::memcpy(pool->list_host + off, offsets_host, (size_t)(n_seqs + 1) * 4);
-    cudaError_t e = cudaMemcpyAsync(pool->list_dev + off, pool->list_host + off, (size_t)(n_seqs + 1) * 4, cudaMemcpyHostToDevice, stream);
+    st = pie_prompt_plan(offsets_host, n_seqs, 2 * tile_tokens, pool->list_host + off, n_items, &n_items);
+    if (st != PIE_OK) return st;   // (nothing is enqueued; the ring's piece is free again)
+    cudaError_t e = cudaMemcpyAsync(pool->list_dev + off, pool->list_host + off, (size_t)n_items * 16, cudaMemcpyHostToDevice, stream);
     if (e == cudaSuccess) {
         pie::PromptLaunch a{};
         a.q = q;
         a.k = k;
         a.v = v;
         a.out = out;
-        a.offsets = pool->list_dev + off;
+        a.items = pool->list_dev + off;
+        a.n_items = n_items;
+        a.tile_tokens = tile_tokens;
         a.q_stride = q_stride;
         a.k_stride = k_stride;
         a.v_stride = v_stride;
         a.n_tokens = n_tokens;
-        a.n_seqs = n_seqs;
         a.scale = scale;
         a.status = pool->status_dev;
         e = pie::launch_prompt_attention(pool_shape(pool), a, stream);
     }
     st = end_layer_work(pool, e, 0);
     if (st == PIE_OK) {
-        st = list_commit(pool, off, n_seqs + 1, stream);
+        st = list_commit(pool, off, 4 * n_items, stream);
         if (st != PIE_OK) pool->sticky = st;
     }
     return st;

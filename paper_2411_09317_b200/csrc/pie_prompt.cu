@@ -1,8 +1,21 @@
 // Causal attention over whole prompts, packed one after the other (Section 2.1: the prefill stage computes all prompt tokens at
-// once): keys and values as the projection left them, nothing cached before them.
+// once), on the fifth-generation tensor cores: keys and values as the projection left them, nothing cached before them.
 //
-// One warp per (token, query head): a lane holds head_dim / 32 elements of the query and of the output, the scores are
-// summed across the lanes, and one pass over the keys carries the running maximum and sum of the softmax.
+// A row is a (token, query head of the KV head's group) pair, token-major.  Work item = (sequence, KV head, two tiles of 128
+// consecutive rows): the two tiles take turns on the tensor core and share every K and V stage, so that one tile's softmax runs
+// while the other's products do, and a stage's 64 KiB (head_dim 128) cross from L2 to the SM once per 256 rows - with one tile
+// per CTA and two CTAs per SM that traffic alone, 64 bytes per clock and SM, is more than L2 delivers.
+//   - The loading warp brings the Q tiles and the K and V stages (128 tokens; TMA tiles of 64 elements, 128-byte swizzle) through
+//     a ring of stage buffers: K0, V0, K1, V1, ...
+//   - One thread of the issuing warp issues the MMAs.  Per tile and stage: S = Q K^T (128 x 128 x D, fp32, 128 TMEM columns) and
+//     O += P V (D TMEM columns) with P read from TMEM.  The order is O0 += P0 V(j), S0(j + 1), O1 += P1 V(j), S1(j + 1): tcgen05
+//     MMAs of one thread complete in order, so S may follow O += P V over the same columns without a wait, and a softmax warp
+//     that sees S(j + 1) knows O += P V of stage j to be complete.
+//   - Eight softmax warps, four per tile, a thread per row: the 128 scores in registers, maximum (three-input), one packed
+//     multiply-add per pair of elements, exponentials, packed sums, P back into TMEM over the scores.
+// Scores and sums in fp32.  P is rounded once to the 16-bit type on its way to the tensor core (a second operand with the
+// rounding remainder, as the chunked kernel has for bf16, costs half as many MMAs again and buys less than the output's own
+// rounding); the row's sum is of the unrounded probabilities.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -10,73 +23,450 @@
 
 #include "../../include/pie.h"
 #include "pie_kernels.h"
+#include "pie_tc.h"
 
 namespace pie {
 
 namespace {
 
+constexpr int PR_KV = 128;                    // tokens of a stage
+constexpr int PR_SOFTMAX_THREADS = 256;       // warps 0 .. 3: tile 0, warps 4 .. 7: tile 1
+constexpr int PR_THREADS = PR_SOFTMAX_THREADS + 64;   // + the issuing warp (8) and the loading warp (9)
+constexpr int PR_TMEM_COLS = 512;             // S0, S1 (128 each; P over them), O0, O1 (128 each)
+// A row's running maximum is raised - and its O and sum rescaled - only when a stage exceeds it by more than this (log2
+// units): probabilities are then at most 2^8, harmless in fp32 sums and in both 16-bit types, and after the first stages
+// hardly any stage rescales.
+constexpr float PR_LAZY = 8.f;
+
+struct PromptParams {
+    const int4 *items;       // {first token of the sequence, first token of the item (within it), sequence length, -}
+    uint16_t *out;
+    const uint16_t *v;       // (the values again, for the rare repair below)
+    int32_t *status;
+    int64_t v_stride;
+    int32_t n_q_heads, n_kv_heads, group, tile_tokens;
+    float scale_log2e;
+};
+
+template <int D>
+struct PrSmem {
+    static constexpr int Q_BYTES = 2 * TC_M * D * 2;   // two tiles of [D / 64][128 rows][128 B]
+    static constexpr int STAGE = PR_KV * D * 2;        // [D / 64][128 tokens][128 B]
+    static constexpr int RING = D == 128 ? 5 : 8;
+    static constexpr int OFF_Q = 0;
+    static constexpr int OFF_RING = OFF_Q + Q_BYTES;
+    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[RING], empty[RING], q, s[2], p[2], done[2]
+    static constexpr int OFF_MISC = OFF_BAR + (2 * RING + 8) * 8;   // [0] TMEM base, [1] abort, [2] a value was not finite
+    static constexpr int BYTES = OFF_MISC + 32;
+};
+
+__device__ __forceinline__ void pr_tma_3d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+
+// the larger of three; NaN if any of them is one
+__device__ __forceinline__ float pr_max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float2 pr_fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(*reinterpret_cast<uint64_t *>(&r))
+        : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+    return r;
+}
+__device__ __forceinline__ float2 pr_add2(float2 a, float2 b) {
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(*reinterpret_cast<uint64_t *>(&r))
+        : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return r;
+}
+
+// largest magnitude bits of the two halves of each word; >= EXP in a half: that value is not finite
 template <bool BF16>
-__device__ __forceinline__ float pr_load(const uint16_t *x) {
-    return BF16 ? __uint_as_float((uint32_t)*x << 16) : __half2float(__ushort_as_half(*x));
+__device__ __forceinline__ bool pr_not_finite(const uint4 &w) {
+    const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+    constexpr uint32_t EXP = BF16 ? 0x7f80u : 0x7c00u;
+    return (m & 0xffffu) >= EXP || (m >> 16) >= EXP;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pr_clear_not_finite(uint32_t w) {
+    constexpr uint32_t EXP = BF16 ? 0x7f80u : 0x7c00u;
+    if ((w & 0x7fffu) >= EXP) w &= 0xffff0000u;
+    if (((w >> 16) & 0x7fffu) >= EXP) w &= 0xffffu;
+    return w;
 }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256)
-prompt_attn_kernel(const PromptLaunch a, int32_t n_q_heads, int32_t n_kv_heads) {
-    const int lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int64_t t = row / n_q_heads;
-    if (t >= a.n_tokens) return;
-    const int h = (int)(row - t * n_q_heads), kvh = h / (n_q_heads / n_kv_heads);
-    int32_t lo = 0, hi = a.n_seqs;   // largest s with offsets[s] <= t
-    while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (a.offsets[mid] <= t) lo = mid;
-        else hi = mid;
+__global__ void __launch_bounds__(PR_THREADS, 1)
+prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, const PromptParams p) {
+    using SM = PrSmem<D>;
+    constexpr int HALVES = D / 64;
+    constexpr int RING = SM::RING;
+    extern __shared__ __align__(1024) uint8_t pr_smem[];
+    uint8_t *smem = pr_smem;
+    const uint32_t base = pf_smem_u32(pr_smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (base & 1023u) {   // the swizzled tiles need a 1024-byte boundary: never seen otherwise, but do not compute garbage
+        if (tid == 0) pf_raise(p.status, STATUS_WAIT_TIMEOUT);
+        return;
     }
-    const int64_t t0 = a.offsets[lo];
-    const uint16_t *q = (const uint16_t *)a.q + t * a.q_stride + (int64_t)h * D;
-    float x[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        x[i] = pr_load<BF16>(q + 32 * i + lane);
-        o[i] = 0.f;
+    const uint32_t bar_full = base + SM::OFF_BAR, bar_empty = bar_full + 8 * RING, bar_q = bar_empty + 8 * RING;
+    const uint32_t bar_s = bar_q + 8, bar_p = bar_s + 16, bar_done = bar_p + 16;
+    volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
+
+    // ---- which rows
+    const int32_t item = blockIdx.x / p.n_kv_heads, kvh = blockIdx.x - item * p.n_kv_heads;
+    const int4 it = __ldg(p.items + item);
+    const int32_t seq0 = it.x, tok0 = it.y, len = it.z;
+    const int32_t G = p.group, TT = p.tile_tokens;
+    // stages of each tile: what its last token sees (a tile behind the sequence's end has none)
+    const int32_t end0 = min(tok0 + TT, len), end1 = min(tok0 + 2 * TT, len);
+    const int32_t n0 = (end0 + PR_KV - 1) / PR_KV, n1 = end1 > end0 ? (end1 + PR_KV - 1) / PR_KV : 0;
+    const int32_t n_stages = max(n0, n1);
+
+    if (tid == 0) {
+        for (int i = 0; i < RING; ++i) {
+            pf_mbar_init(bar_full + 8 * i, 1);
+            pf_mbar_init(bar_empty + 8 * i, 1);
+        }
+        pf_mbar_init(bar_q, 1);
+        for (int t = 0; t < 2; ++t) {
+            pf_mbar_init(bar_s + 8 * t, 1);
+            pf_mbar_init(bar_p + 8 * t, 128);
+            pf_mbar_init(bar_done + 8 * t, 1);
+        }
+        misc[1] = 0;
+        misc[2] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    for (int64_t j = t0; j <= t; ++j) {
-        const uint16_t *k = (const uint16_t *)a.k + j * a.k_stride + (int64_t)kvh * D, *v = (const uint16_t *)a.v + j * a.v_stride + (int64_t)kvh * D;
-        float s = 0.f;
+    if (warp == 8) tmem_alloc(base + SM::OFF_MISC, PR_TMEM_COLS);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = misc[0];
+
+    auto dead = [&]() { return __shfl_sync(0xffffffffu, misc[1] != 0 ? 1 : 0, 0) != 0; };
+    auto wait_all = [&](uint32_t bar, uint32_t parity) {   // by every lane of a warp; false: give up
+        if (!pf_mbar_wait(bar, parity)) {
+            pf_raise(p.status, STATUS_WAIT_TIMEOUT);
+            misc[1] = 1;
+        }
+        __syncwarp();
+        return !dead();
+    };
+
+    if (warp == 9) {
+        // =============================================================================== the loading warp
+        // Ring entry i holds K (even i) or V (odd i) of stage i / 2.
+        const uint32_t q_rows = (uint32_t)(G * TT);
+        if (lane == 0) {
+            const int tiles = n1 > 0 ? 2 : 1;
+            pf_mbar_expect_tx(bar_q, tiles * q_rows * D * 2);
+            for (int t = 0; t < tiles; ++t)
+                for (int h = 0; h < HALVES; ++h)
+                    pr_tma_3d(base + SM::OFF_Q + t * (TC_M * D * 2) + h * (TC_M * 128), &map_q, 64 * h, kvh * G, seq0 + tok0 + t * TT, bar_q);
+        }
+        __syncwarp();
+        int32_t issued = 0;
+        for (int32_t i = 0; i < 2 * n_stages; ++i) {
+            const uint32_t slot = (uint32_t)(i % RING);
+            if (i >= RING && !wait_all(bar_empty + 8 * slot, (uint32_t)((i / RING - 1) & 1))) break;
+            if (lane == 0) {
+                pf_mbar_expect_tx(bar_full + 8 * slot, SM::STAGE);
+                for (int h = 0; h < HALVES; ++h)
+                    pr_tma_3d(base + SM::OFF_RING + slot * SM::STAGE + h * (PR_KV * 128), (i & 1) ? &map_v : &map_k, 64 * h, kvh,
+                              seq0 + (i >> 1) * PR_KV, bar_full + 8 * slot);
+            }
+            __syncwarp();
+            issued = i + 1;
+        }
+        if (dead()) {   // giving up: wait (bounded) for the copies that still write into this CTA's shared memory
+            pf_mbar_wait(bar_q, 0);
+            for (int32_t i = max(0, issued - RING); i < issued; ++i) pf_mbar_wait(bar_full + 8 * (i % RING), (uint32_t)((i / RING) & 1));
+        }
+        __syncwarp();
+    } else if (warp == 8) {
+        // =============================================================================== the issuing warp
+        constexpr uint32_t IDESC_S = instr_desc(BF16, PR_KV, false), IDESC_O = instr_desc(BF16, D, true);
+        // S of a tile and stage
+        auto issue_s = [&](int t, int32_t j) {
+            const uint32_t slot = (uint32_t)((2 * j) % RING);
+            const uint32_t k0 = base + SM::OFF_RING + slot * SM::STAGE, q0 = base + SM::OFF_Q + t * (TC_M * D * 2);
+            if (lane == 0) {
+                tc_fence_after();
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) s += x[i] * pr_load<BF16>(k + 32 * i + lane);
+                for (int ks = 0; ks < D / 16; ++ks)
+                    mma_f16(tmem + t * 128, smem_desc(q0 + (ks >> 2) * (TC_M * 128) + (ks & 3) * 32, 16, 1024),
+                            smem_desc(k0 + (ks >> 2) * (PR_KV * 128) + (ks & 3) * 32, 16, 1024), IDESC_S, ks > 0 ? 1u : 0u);
+                tc_commit(bar_s + 8 * t);
+            }
+            __syncwarp();
+        };
+        auto release = [&](int32_t i) {   // ring entry i: free once everything issued so far is complete
+            if (lane == 0) tc_commit(bar_empty + 8 * (uint32_t)(i % RING));
+            __syncwarp();
+        };
+        bool ok = wait_all(bar_q, 0) && wait_all(bar_full, 0);
+        if (ok) {
+            issue_s(0, 0);
+            if (n1 > 0) issue_s(1, 0);
+            release(0);
+        }
+        for (int32_t j = 0; ok && j < n_stages; ++j) {
+            const int32_t iv = 2 * j + 1, ik = 2 * j + 2;
+            const uint32_t v0 = base + SM::OFF_RING + (uint32_t)(iv % RING) * SM::STAGE;
+            ok = wait_all(bar_full + 8 * (iv % RING), (uint32_t)((iv / RING) & 1));
+            bool k_there = false;
 #pragma unroll
-        for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        s *= a.scale * 1.4426950408889634f;
-        const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : exp2f(m - mn), e = mn == -INFINITY ? 0.f : exp2f(s - mn);
-        m = mn;
-        l = l * f + e;
+            for (int t = 0; t < 2; ++t) {
+                const int32_t n = t == 0 ? n0 : n1;
+                if (!ok || j >= n) continue;
+                ok = wait_all(bar_p + 8 * t, (uint32_t)(j & 1));
+                if (!ok) continue;
+                if (lane == 0) {
+                    tc_fence_after();
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) o[i] = o[i] * f + e * pr_load<BF16>(v + 32 * i + lane);
+                    for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
+                        mma_f16_ts(tmem + 256 + t * 128, tmem + t * 128 + ks * 8, smem_desc(v0 + ks * 2048, PR_KV * 128, 1024), IDESC_O,
+                                   (j > 0 || ks > 0) ? 1u : 0u);
+                    if (j + 1 == n) tc_commit(bar_done + 8 * t);
+                }
+                __syncwarp();
+                if (j + 1 < n) {
+                    if (!k_there) ok = wait_all(bar_full + 8 * (ik % RING), (uint32_t)((ik / RING) & 1));
+                    k_there = true;
+                    if (ok) issue_s(t, j + 1);
+                }
+            }
+            if (ok) {
+                release(iv);
+                if (j + 1 < n_stages) release(ik);
+            }
+        }
+        __syncwarp();
+    } else {
+        // =============================================================================== the softmax warps
+        const int t = warp >> 2;
+        const int r = tid & 127;                                      // row of the tile
+        const int32_t n = t == 0 ? n0 : n1;
+        const int32_t my_tok = r / G, my_g = r - my_tok * G;
+        const int32_t first = tok0 + t * TT;                          // the tile's first position
+        const int32_t my_pos = first + my_tok;
+        const bool row_valid = my_tok < TT && my_pos < len;
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tmem_s = tmem + t * 128 + lane_addr, tmem_o = tmem + 256 + t * 128 + lane_addr;
+        float m_run = -INFINITY, l_run = 0.f;
+        bool spoiled = false;                                         // a score the row sees is NaN or +inf: so is the softmax
+        bool ok = true;
+        for (int32_t j = 0; j < n; ++j) {
+            if (!wait_all(bar_s + 8 * t, (uint32_t)(j & 1))) { ok = false; break; }
+            tc_fence_after();
+            uint32_t sv[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(tmem_s + 32 * c, sv[c]);
+            tmem_wait_ld();
+            const int32_t t_base = j * PR_KV;
+            const bool masked = t_base + PR_KV - 1 > first;           // some row of the tile does not see the whole stage
+            float scale = p.scale_log2e;
+            if (masked || scale <= 0.f) {
+                // scores in log2 units, what a row may not see at -inf (by selection: NaN scores too)
+#pragma unroll
+                for (int c = 0; c < 128; ++c) {
+                    const float x = __uint_as_float(sv[c >> 5][c & 31]) * scale;
+                    sv[c >> 5][c & 31] = __float_as_uint(t_base + c <= my_pos ? x : -INFINITY);
+                }
+                scale = 1.f;
+            }
+            float a0 = -INFINITY, a1 = -INFINITY, a2 = -INFINITY, a3 = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+                a0 = pr_max3(a0, __uint_as_float(sv[0][c]), __uint_as_float(sv[0][c + 1]));
+                a1 = pr_max3(a1, __uint_as_float(sv[1][c]), __uint_as_float(sv[1][c + 1]));
+                a2 = pr_max3(a2, __uint_as_float(sv[2][c]), __uint_as_float(sv[2][c + 1]));
+                a3 = pr_max3(a3, __uint_as_float(sv[3][c]), __uint_as_float(sv[3][c + 1]));
+            }
+            const float mx = pr_max3(a0, a1, pr_max3(a2, a3, a3)) * scale;
+            spoiled |= !(mx < INFINITY);
+            const float m_cand = fmaxf(m_run, mx);
+            const bool grow = m_cand > m_run + PR_LAZY;               // (m_run = -inf: true unless the row has seen nothing finite yet)
+            const float m_new = grow ? m_cand : m_run;
+            const float alpha = grow ? pf_exp2(m_run - m_cand) : 1.f; // (m_run = -inf gives 0: nothing accumulated yet)
+            m_run = m_new;
+            const float neg_m = m_new == -INFINITY ? 0.f : -m_new;    // (a row that has seen nothing: exponents stay -inf)
+            const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(neg_m, neg_m);
+            float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t pw[32];
+#pragma unroll
+                for (int w = 0; w < 32; ++w) {
+                    const int c = 64 * h + 2 * w;
+                    const float2 x = pr_fma2(make_float2(__uint_as_float(sv[c >> 5][c & 31]), __uint_as_float(sv[c >> 5][(c & 31) + 1])), sc2, nm2);
+                    const float2 e = make_float2(pf_exp2(x.x), pf_exp2(x.y));
+                    if (w & 1) s1 = pr_add2(s1, e);
+                    else s0 = pr_add2(s0, e);
+                    pw[w] = pf_pack2<BF16>(e.x, e.y);
+                }
+                tmem_st32(tmem_s + 32 * h, pw);   // a thread overwrites only its own row's scores, which it has read
+            }
+            s0 = pr_add2(s0, s1);
+            l_run = l_run * alpha + (s0.x + s0.y);
+            // ---- O *= alpha where a row's maximum moved (skipped by warps in which none did)
+            if (j >= 1 && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    uint32_t ov[32];
+                    tmem_ld32(tmem_o + c0, ov);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * alpha);
+                    tmem_st32(tmem_o + c0, ov);
+                }
+            }
+            if (masked) {
+                // Values that some row of the item may not see meet P = 0 there, which hides everything but NaN and infinities.
+                // Those are cleared in the stage and, if there were any, added at the end to the rows that do see them.
+                const int32_t iv = 2 * j + 1;
+                if (!wait_all(bar_full + 8 * (iv % RING), (uint32_t)((iv / RING) & 1))) { ok = false; break; }
+                uint8_t *vs = smem + SM::OFF_RING + (iv % RING) * SM::STAGE;
+                const int row_first = max(0, tok0 + 1 - t_base);
+                bool found = false;
+                for (int e = row_first * 8 + r; e < PR_KV * 8; e += 128)
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) {
+                        uint4 *at = reinterpret_cast<uint4 *>(vs + h * (PR_KV * 128) + e * 16);
+                        uint4 w = *at;
+                        if (pr_not_finite<BF16>(w)) {
+                            found = true;
+                            w.x = pr_clear_not_finite<BF16>(w.x);
+                            w.y = pr_clear_not_finite<BF16>(w.y);
+                            w.z = pr_clear_not_finite<BF16>(w.z);
+                            w.w = pr_clear_not_finite<BF16>(w.w);
+                            *at = w;
+                        }
+                    }
+                if (found) misc[2] = 1;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            pf_mbar_arrive(bar_p + 8 * t);
+        }
+        if (ok && n > 0) ok = wait_all(bar_done + 8 * t, 0u);
+        // ---- out = O / l, rounded to the 16-bit type (nearest even).  The TMEM loads are warp-wide: rows beyond the tile take
+        // part in them and store nothing.
+        if (ok && n > 0) {
+            tc_fence_after();
+            const float inv = spoiled ? __int_as_float(0x7fc00000) : 1.f / l_run;
+            const bool repair = misc[2] != 0;
+            uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((int64_t)(seq0 + my_pos) * p.n_q_heads + kvh * G + my_g) * D);
+            const uint16_t *vrow = p.v + (int64_t)(seq0 + tok0 + 1) * p.v_stride + (int64_t)kvh * D;
+#pragma unroll 1
+            for (int c0 = 0; c0 < D; c0 += 32) {
+                uint32_t ov[32];
+                tmem_ld32(tmem_o + c0, ov);
+                tmem_wait_ld();
+                if (row_valid) {
+                    if (repair) {
+                        for (int32_t k = 0; tok0 + 1 + k <= my_pos; ++k)
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                const uint32_t b = vrow[k * p.v_stride + c0 + c];
+                                const float x = BF16 ? __uint_as_float(b << 16) : __half2float(__ushort_as_half((uint16_t)b));
+                                if ((b & 0x7fffu) >= (BF16 ? 0x7f80u : 0x7c00u)) ov[c] = __float_as_uint(__uint_as_float(ov[c]) + x);
+                            }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 8) {
+                        uint4 v;
+                        v.x = pf_pack2<BF16>(__uint_as_float(ov[c]) * inv, __uint_as_float(ov[c + 1]) * inv);
+                        v.y = pf_pack2<BF16>(__uint_as_float(ov[c + 2]) * inv, __uint_as_float(ov[c + 3]) * inv);
+                        v.z = pf_pack2<BF16>(__uint_as_float(ov[c + 4]) * inv, __uint_as_float(ov[c + 5]) * inv);
+                        v.w = pf_pack2<BF16>(__uint_as_float(ov[c + 6]) * inv, __uint_as_float(ov[c + 7]) * inv);
+                        dst[(c0 + c) >> 3] = v;
+                    }
+                }
+            }
+        }
     }
-    uint16_t *out = (uint16_t *)a.out + (t * n_q_heads + h) * D;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const float r = o[i] / l;
-        out[32 * i + lane] = BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(r)) : __half_as_ushort(__float2half_rn(r));
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem, PR_TMEM_COLS);
+}
+
+// [tokens][heads][head_dim] as tiles of 64 elements x `heads` heads x `tokens` tokens
+cudaError_t make_token_map(const void *x, int64_t n_tokens, int64_t stride, int n_heads, int head_dim, int box_heads, int box_tokens,
+                           CUtensorMap *map) {
+    typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                      const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static EncodeTiledFn encode = nullptr;
+    if (!encode) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+        if (e != cudaSuccess) return e;
+        if (fn == nullptr || qres != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+        encode = reinterpret_cast<EncodeTiledFn>(fn);
     }
+    cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)n_heads, (cuuint64_t)n_tokens};
+    cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)stride * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(x), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <typename F>
+cudaError_t dispatch_prompt(int head_dim, int dtype, F &&f) {
+    if (head_dim == 128) return dtype == PIE_BF16 ? f(prompt_attn_kernel<128, true>, PrSmem<128>::BYTES) : f(prompt_attn_kernel<128, false>, PrSmem<128>::BYTES);
+    return dtype == PIE_BF16 ? f(prompt_attn_kernel<64, true>, PrSmem<64>::BYTES) : f(prompt_attn_kernel<64, false>, PrSmem<64>::BYTES);
 }
 
 }  // namespace
 
+cudaError_t prompt_configure(int head_dim, int dtype) {
+    return dispatch_prompt(head_dim, dtype, [](auto kernel, int smem) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    });
+}
+
 cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, cudaStream_t stream) {
-    if (a.n_tokens <= 0) return cudaSuccess;
-    const unsigned grid = (unsigned)((a.n_tokens * sh.n_q_heads + 7) / 8);
-    if (sh.dtype == PIE_BF16) {
-        if (sh.head_dim == 128) prompt_attn_kernel<128, true><<<grid, 256, 0, stream>>>(a, sh.n_q_heads, sh.n_kv_heads);
-        else prompt_attn_kernel<64, true><<<grid, 256, 0, stream>>>(a, sh.n_q_heads, sh.n_kv_heads);
-    } else {
-        if (sh.head_dim == 128) prompt_attn_kernel<128, false><<<grid, 256, 0, stream>>>(a, sh.n_q_heads, sh.n_kv_heads);
-        else prompt_attn_kernel<64, false><<<grid, 256, 0, stream>>>(a, sh.n_q_heads, sh.n_kv_heads);
-    }
-    return cudaGetLastError();
+    if (a.n_items <= 0) return cudaSuccess;
+    const int group = sh.n_q_heads / sh.n_kv_heads;
+    CUtensorMap map_q, map_k, map_v;
+    cudaError_t e = make_token_map(a.q, a.n_tokens, a.q_stride, sh.n_q_heads, sh.head_dim, group, a.tile_tokens, &map_q);
+    if (e == cudaSuccess) e = make_token_map(a.k, a.n_tokens, a.k_stride, sh.n_kv_heads, sh.head_dim, 1, PR_KV, &map_k);
+    if (e == cudaSuccess) e = make_token_map(a.v, a.n_tokens, a.v_stride, sh.n_kv_heads, sh.head_dim, 1, PR_KV, &map_v);
+    if (e != cudaSuccess) return e;
+    PromptParams p;
+    p.items = reinterpret_cast<const int4 *>(a.items);
+    p.out = (uint16_t *)a.out;
+    p.v = (const uint16_t *)a.v;
+    p.status = a.status;
+    p.v_stride = a.v_stride;
+    p.n_q_heads = sh.n_q_heads;
+    p.n_kv_heads = sh.n_kv_heads;
+    p.group = group;
+    p.tile_tokens = a.tile_tokens;
+    p.scale_log2e = a.scale * 1.4426950408889634f;
+    return dispatch_prompt(sh.head_dim, sh.dtype, [&](auto kernel, int smem) {
+        kernel<<<(unsigned)(a.n_items * sh.n_kv_heads), PR_THREADS, smem, stream>>>(map_q, map_k, map_v, p);
+        return cudaGetLastError();
+    });
 }
 
 }  // namespace pie

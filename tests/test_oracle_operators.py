@@ -91,6 +91,28 @@ def test_rope_plan_refuses(args, status):
     assert e.value.status == status
 
 
+@pytest.mark.parametrize("lens", [[1], [0, 0], [64, 65, 0, 1, 1000, 64], [5] * 40, [100000, 3]])
+@pytest.mark.parametrize("item", [64, 256, 84])
+def test_prompt_plan_covers_every_token_once_longest_first(lens, item):
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    items = pie.pie_prompt_plan(off, item)
+    seen = np.zeros(int(off[-1]), np.int32)
+    for first, tok, n, s in items:
+        assert first == off[s] and n == lens[s] and tok % item == 0 and tok < n
+        seen[first + tok:first + min(tok + item, n)] += 1
+    assert np.all(seen == 1)
+    assert np.all(np.diff(items[:, 1]) <= 0)          # an item sees the keys up to its last token: the longest first
+
+
+@pytest.mark.parametrize("off", [[1, 2], [0, 5, 4], [0, -1]])
+def test_prompt_plan_refuses(off):
+    with pytest.raises(pie.PieError) as e:
+        pie.pie_prompt_plan(off, 64)
+    assert e.value.status == pie.PIE_ERR_INVALID
+    with pytest.raises(pie.PieError):
+        pie.pie_prompt_plan([0, 5], 0)
+
+
 def test_calls_without_a_pool_are_refused():
     i, u = pie.PIE_ERR_INVALID, np.zeros(4, np.int32)
     for call in (lambda: pie.pie_set_rope(None, 16, [0] * 8, [1.0] * 8),
