@@ -31,7 +31,14 @@ namespace {
 
 constexpr int PR_KV = 128;                    // tokens of a stage
 constexpr int PR_SOFTMAX_THREADS = 256;       // warps 0 .. 3: tile 0, warps 4 .. 7: tile 1
-constexpr int PR_THREADS = PR_SOFTMAX_THREADS + 64;   // + the issuing warp (8) and the loading warp (9)
+constexpr int PR_THREADS = PR_SOFTMAX_THREADS + 128;  // + the issuing warp (8), the loading warp (9) and two that only give registers
+// Registers: 384 threads get 168 each at launch; the softmax warpgroups, whose threads hold a row of 128 scores, take over what
+// the third gives up: 2 x 128 x 208 + 128 x 88 = 384 x 168.
+constexpr int PR_REGS_SOFTMAX = 208, PR_REGS_REST = 88;
+static_assert(2 * PR_REGS_SOFTMAX + PR_REGS_REST == 3 * 168, "what one side takes the other gives");
+#ifndef PR_POLY
+#define PR_POLY 2
+#endif
 constexpr int PR_TMEM_COLS = 512;             // S0, S1 (128 each; P over them), O0, O1 (128 each)
 // A row's running maximum is raised - and its O and sum rescaled - only when a stage exceeds it by more than this (log2
 // units): probabilities are then at most 2^8, harmless in fp32 sums and in both 16-bit types, and after the first stages
@@ -55,8 +62,8 @@ struct PrSmem {
     static constexpr int RING = D == 128 ? 5 : 8;
     static constexpr int OFF_Q = 0;
     static constexpr int OFF_RING = OFF_Q + Q_BYTES;
-    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[RING], empty[RING], q, s[2], p[2], done[2]
-    static constexpr int OFF_MISC = OFF_BAR + (2 * RING + 8) * 8;   // [0] TMEM base, [1] abort, [2] a value was not finite
+    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], s[2 tiles][2 parities], p[2], done[2], q
+    static constexpr int OFF_MISC = OFF_BAR + 16 * 8;         // [0] TMEM base, [1] abort, [2] a value was not finite
     static constexpr int BYTES = OFF_MISC + 32;
 };
 
@@ -64,6 +71,34 @@ __device__ __forceinline__ void pr_tma_3d(uint32_t dst, const CUtensorMap *map, 
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+
+// tcgen05.mma / commit by the lane whose `leader` is not 0, without a branch
+__device__ __forceinline__ void pr_mma_ss(uint32_t leader, uint32_t tmem_d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void pr_mma_ts(uint32_t leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void pr_commit(uint32_t leader, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t"
+        "setp.ne.b32 e, %1, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+        ::"r"(bar), "r"(leader)
         : "memory");
 }
 
@@ -86,6 +121,24 @@ __device__ __forceinline__ float2 pr_add2(float2 a, float2 b) {
         : "=l"(*reinterpret_cast<uint64_t *>(&r))
         : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
     return r;
+}
+
+// 2^x for two values at once, in the arithmetic pipes instead of the special-function unit: 2^round(x) by the exponent field, 2^f
+// for the remaining |f| <= 1/2 by the polynomial of degree 3 with the least relative error there (7.5e-5, from a Remez
+// iteration: an eighth of bf16's half step and a sixth of fp16's).  Below -125 it stays at 2^-125.
+__device__ __forceinline__ float2 pr_exp2_poly(float2 x) {
+    x.x = fmaxf(x.x, -125.f);
+    x.y = fmaxf(x.y, -125.f);
+    const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);
+    const float2 t = pr_add2(x, magic);            // the rounded value in the low bits
+    const float2 n = pr_add2(t, unmagic);
+    const float2 f = pr_fma2(n, make_float2(-1.f, -1.f), x);
+    float2 y = pr_fma2(f, make_float2(0.0551716685f, 0.0551716685f), make_float2(0.242611125f, 0.242611125f));
+    y = pr_fma2(y, f, make_float2(0.693260968f, 0.693260968f));
+    y = pr_fma2(y, f, make_float2(0.999928057f, 0.999928057f));
+    y.x = __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
+    y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
+    return y;
 }
 
 // largest magnitude bits of the two halves of each word; >= EXP in a half: that value is not finite
@@ -118,8 +171,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (tid == 0) pf_raise(p.status, STATUS_WAIT_TIMEOUT);
         return;
     }
-    const uint32_t bar_full = base + SM::OFF_BAR, bar_empty = bar_full + 8 * RING, bar_q = bar_empty + 8 * RING;
-    const uint32_t bar_s = bar_q + 8, bar_p = bar_s + 16, bar_done = bar_p + 16;
+    // Full barriers: one for Q and K(0), then one for every V(j) with K(j + 1), four in turn.  There are no empty barriers: what
+    // a ring entry held has been used when the scores of a later stage are complete (MMAs of one thread complete in order), so the
+    // loading warp waits for those.  It may be a stage behind the softmax warps, hence the scores' barriers by stage parity (a
+    // parity wait may be at most one phase behind).
+    const uint32_t bar_full = base + SM::OFF_BAR, bar_s = bar_full + 32, bar_p = bar_s + 32, bar_done = bar_p + 16, bar_q = bar_done + 16;
+    auto bar_scores = [&](int t, int32_t j) { return bar_s + 16 * t + 8 * (j & 1); };
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
 
     // ---- which rows
@@ -133,13 +190,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const int32_t n_stages = max(n0, n1);
 
     if (tid == 0) {
-        for (int i = 0; i < RING; ++i) {
+        for (int i = 0; i < 4; ++i) {
             pf_mbar_init(bar_full + 8 * i, 1);
-            pf_mbar_init(bar_empty + 8 * i, 1);
+            pf_mbar_init(bar_s + 8 * i, 1);
         }
         pf_mbar_init(bar_q, 1);
         for (int t = 0; t < 2; ++t) {
-            pf_mbar_init(bar_s + 8 * t, 1);
             pf_mbar_init(bar_p + 8 * t, 128);
             pf_mbar_init(bar_done + 8 * t, 1);
         }
@@ -153,108 +209,123 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = misc[0];
+    if (tmem != 0 && tid == 0) {   // (every column is this CTA's: cannot be) - the issuing warp goes by it
+        pf_raise(p.status, STATUS_WAIT_TIMEOUT);
+        misc[1] = 1;
+    }
 
-    auto dead = [&]() { return __shfl_sync(0xffffffffu, misc[1] != 0 ? 1 : 0, 0) != 0; };
-    auto wait_all = [&](uint32_t bar, uint32_t parity) {   // by every lane of a warp; false: give up
-        if (!pf_mbar_wait(bar, parity)) {
+    auto dead = [&]() { return __any_sync(0xffffffffu, misc[1] != 0); };
+    // by every lane of a warp; false: give up (the wait ran out, here or in another warp).  Bounded: about a second.
+    auto wait_all = [&](uint32_t bar, uint32_t parity) {
+        if (pf_mbar_try_wait(bar, parity)) {
+            __syncwarp();
+            return true;
+        }
+        bool there = false;
+        for (uint32_t i = 0; i < (1u << 22) && !there; ++i) {
+            there = pf_mbar_try_wait(bar, parity);
+            if (!there && i > 64) {
+                if (misc[1] != 0) break;
+                __nanosleep(200);
+            }
+        }
+        if (!there) {
             pf_raise(p.status, STATUS_WAIT_TIMEOUT);
             misc[1] = 1;
         }
-        __syncwarp();
-        return !dead();
+        return __all_sync(0xffffffffu, there) != 0;
     };
 
+    // (each role's own branch holds its register instruction: the compiler allocates by region)
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_REST));
     if (warp == 9) {
         // =============================================================================== the loading warp
-        // Ring entry i holds K (even i) or V (odd i) of stage i / 2.
-        const uint32_t q_rows = (uint32_t)(G * TT);
+        // Ring entry i (slot i % RING) holds K (even i) or V (odd i) of stage i / 2.
+        auto load = [&](int32_t i, uint32_t bar) {
+            const uint32_t dst = base + SM::OFF_RING + (uint32_t)(i % RING) * SM::STAGE;
+            for (int h = 0; h < HALVES; ++h)
+                pr_tma_3d(dst + h * (PR_KV * 128), (i & 1) ? &map_v : &map_k, 64 * h, kvh, seq0 + (i >> 1) * PR_KV, bar);
+        };
+        const int last = n1 > 0 ? 1 : 0;
         if (lane == 0) {
-            const int tiles = n1 > 0 ? 2 : 1;
-            pf_mbar_expect_tx(bar_q, tiles * q_rows * D * 2);
-            for (int t = 0; t < tiles; ++t)
+            const uint32_t q_rows = (uint32_t)(G * TT);
+            pf_mbar_expect_tx(bar_q, (last + 1) * q_rows * D * 2 + SM::STAGE);
+            for (int t = 0; t <= last; ++t)
                 for (int h = 0; h < HALVES; ++h)
                     pr_tma_3d(base + SM::OFF_Q + t * (TC_M * D * 2) + h * (TC_M * 128), &map_q, 64 * h, kvh * G, seq0 + tok0 + t * TT, bar_q);
+            load(0, bar_q);
         }
         __syncwarp();
         int32_t issued = 0;
-        for (int32_t i = 0; i < 2 * n_stages; ++i) {
-            const uint32_t slot = (uint32_t)(i % RING);
-            if (i >= RING && !wait_all(bar_empty + 8 * slot, (uint32_t)((i / RING - 1) & 1))) break;
+        for (int32_t j = 0; j < n_stages; ++j) {   // V(j) and K(j + 1)
+            // the slots' entries before: 2 j + 1 - RING and 2 j + 2 - RING, of which the newer was used by the scores of this stage
+            // (a K) or by an O += P V that they follow (a V)
+            const int32_t used = (2 * j + 3 - RING) / 2;
+            if (2 * j + 2 >= RING && !wait_all(bar_scores(last, used), (uint32_t)((used >> 1) & 1))) break;
             if (lane == 0) {
-                pf_mbar_expect_tx(bar_full + 8 * slot, SM::STAGE);
-                for (int h = 0; h < HALVES; ++h)
-                    pr_tma_3d(base + SM::OFF_RING + slot * SM::STAGE + h * (PR_KV * 128), (i & 1) ? &map_v : &map_k, 64 * h, kvh,
-                              seq0 + (i >> 1) * PR_KV, bar_full + 8 * slot);
+                const uint32_t bar = bar_full + 8 * (j & 3);
+                pf_mbar_expect_tx(bar, j + 1 < n_stages ? 2 * SM::STAGE : SM::STAGE);
+                load(2 * j + 1, bar);
+                if (j + 1 < n_stages) load(2 * j + 2, bar);
             }
             __syncwarp();
-            issued = i + 1;
+            issued = j + 1;
         }
         if (dead()) {   // giving up: wait (bounded) for the copies that still write into this CTA's shared memory
             pf_mbar_wait(bar_q, 0);
-            for (int32_t i = max(0, issued - RING); i < issued; ++i) pf_mbar_wait(bar_full + 8 * (i % RING), (uint32_t)((i / RING) & 1));
+            for (int32_t j = max(0, issued - 4); j < issued; ++j) pf_mbar_wait(bar_full + 8 * (j & 3), (uint32_t)((j >> 2) & 1));
         }
         __syncwarp();
     } else if (warp == 8) {
         // =============================================================================== the issuing warp
+        // The descriptors are warp-uniform values, formed outside of any divergent branch (the instruction takes them from uniform
+        // registers: formed in the branch of one lane, each MMA waited some 30 cycles for the moves), and the lane that issues is a
+        // predicate of the instruction.  TMEM: all 512 columns are this CTA's, so its base is column 0.
         constexpr uint32_t IDESC_S = instr_desc(BF16, PR_KV, false), IDESC_O = instr_desc(BF16, D, true);
-        // S of a tile and stage
-        auto issue_s = [&](int t, int32_t j) {
-            const uint32_t slot = (uint32_t)((2 * j) % RING);
-            const uint32_t k0 = base + SM::OFF_RING + slot * SM::STAGE, q0 = base + SM::OFF_Q + t * (TC_M * D * 2);
-            if (lane == 0) {
-                tc_fence_after();
+        const uint32_t leader = lane == 0 ? 1u : 0u;
+        const uint64_t q_desc = smem_desc(base + SM::OFF_Q, 16, 1024), k_desc = smem_desc(base + SM::OFF_RING, 16, 1024);
+        const uint64_t v_desc = smem_desc(base + SM::OFF_RING, PR_KV * 128, 1024);
+        // S of a tile and stage, K in ring slot `slot`
+        auto issue_s = [&](int t, int32_t j, uint32_t slot) {
+            tc_fence_after();
+            const uint64_t qd = q_desc + (uint64_t)(t * (TC_M * D * 2) >> 4), kd = k_desc + (uint64_t)(slot * (SM::STAGE >> 4));
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-                    mma_f16(tmem + t * 128, smem_desc(q0 + (ks >> 2) * (TC_M * 128) + (ks & 3) * 32, 16, 1024),
-                            smem_desc(k0 + (ks >> 2) * (PR_KV * 128) + (ks & 3) * 32, 16, 1024), IDESC_S, ks > 0 ? 1u : 0u);
-                tc_commit(bar_s + 8 * t);
-            }
-            __syncwarp();
+            for (int ks = 0; ks < D / 16; ++ks)
+                pr_mma_ss(leader, t * 128, qd + (uint64_t)(((ks >> 2) * (TC_M * 128) + (ks & 3) * 32) >> 4),
+                          kd + (uint64_t)(((ks >> 2) * (PR_KV * 128) + (ks & 3) * 32) >> 4), IDESC_S, ks > 0 ? 1u : 0u);
+            pr_commit(leader, bar_scores(t, j));
         };
-        auto release = [&](int32_t i) {   // ring entry i: free once everything issued so far is complete
-            if (lane == 0) tc_commit(bar_empty + 8 * (uint32_t)(i % RING));
-            __syncwarp();
-        };
-        bool ok = wait_all(bar_q, 0) && wait_all(bar_full, 0);
+        bool ok = wait_all(bar_q, 0);
         if (ok) {
-            issue_s(0, 0);
-            if (n1 > 0) issue_s(1, 0);
-            release(0);
+            issue_s(0, 0, 0);
+            if (n1 > 0) issue_s(1, 0, 0);
         }
+        uint32_t v_slot = 1;
         for (int32_t j = 0; ok && j < n_stages; ++j) {
-            const int32_t iv = 2 * j + 1, ik = 2 * j + 2;
-            const uint32_t v0 = base + SM::OFF_RING + (uint32_t)(iv % RING) * SM::STAGE;
-            ok = wait_all(bar_full + 8 * (iv % RING), (uint32_t)((iv / RING) & 1));
-            bool k_there = false;
+            const uint32_t k_slot = v_slot + 1 == RING ? 0 : v_slot + 1;
+            const uint64_t vd = v_desc + (uint64_t)(v_slot * (SM::STAGE >> 4));
+            ok = wait_all(bar_full + 8 * (j & 3), (uint32_t)((j >> 2) & 1));   // V(j) and K(j + 1) have landed
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int32_t n = t == 0 ? n0 : n1;
                 if (!ok || j >= n) continue;
                 ok = wait_all(bar_p + 8 * t, (uint32_t)(j & 1));
                 if (!ok) continue;
-                if (lane == 0) {
-                    tc_fence_after();
+                tc_fence_after();
 #pragma unroll
-                    for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
-                        mma_f16_ts(tmem + 256 + t * 128, tmem + t * 128 + ks * 8, smem_desc(v0 + ks * 2048, PR_KV * 128, 1024), IDESC_O,
-                                   (j > 0 || ks > 0) ? 1u : 0u);
-                    if (j + 1 == n) tc_commit(bar_done + 8 * t);
-                }
-                __syncwarp();
-                if (j + 1 < n) {
-                    if (!k_there) ok = wait_all(bar_full + 8 * (ik % RING), (uint32_t)((ik / RING) & 1));
-                    k_there = true;
-                    if (ok) issue_s(t, j + 1);
-                }
+                for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
+                    pr_mma_ts(leader, 256 + t * 128, t * 128 + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), IDESC_O, (j > 0 || ks > 0) ? 1u : 0u);
+                if (j + 1 == n) pr_commit(leader, bar_done + 8 * t);
+                else issue_s(t, j + 1, k_slot);
             }
-            if (ok) {
-                release(iv);
-                if (j + 1 < n_stages) release(ik);
-            }
+            v_slot = k_slot + 1 == RING ? 0 : k_slot + 1;
         }
         __syncwarp();
+    }
     } else {
         // =============================================================================== the softmax warps
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PR_REGS_SOFTMAX));
         const int t = warp >> 2;
         const int r = tid & 127;                                      // row of the tile
         const int32_t n = t == 0 ? n0 : n1;
@@ -268,7 +339,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         bool spoiled = false;                                         // a score the row sees is NaN or +inf: so is the softmax
         bool ok = true;
         for (int32_t j = 0; j < n; ++j) {
-            if (!wait_all(bar_s + 8 * t, (uint32_t)(j & 1))) { ok = false; break; }
+            if (!wait_all(bar_scores(t, j), (uint32_t)((j >> 1) & 1))) { ok = false; break; }
             tc_fence_after();
             uint32_t sv[4][32];
 #pragma unroll
@@ -311,7 +382,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (int w = 0; w < 32; ++w) {
                     const int c = 64 * h + 2 * w;
                     const float2 x = pr_fma2(make_float2(__uint_as_float(sv[c >> 5][c & 31]), __uint_as_float(sv[c >> 5][(c & 31) + 1])), sc2, nm2);
-                    const float2 e = make_float2(pf_exp2(x.x), pf_exp2(x.y));
+                    const float2 e = (w & 7) < PR_POLY ? pr_exp2_poly(x) : make_float2(pf_exp2(x.x), pf_exp2(x.y));
                     if (w & 1) s1 = pr_add2(s1, e);
                     else s0 = pr_add2(s0, e);
                     pw[w] = pf_pack2<BF16>(e.x, e.y);
@@ -336,7 +407,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 // Values that some row of the item may not see meet P = 0 there, which hides everything but NaN and infinities.
                 // Those are cleared in the stage and, if there were any, added at the end to the rows that do see them.
                 const int32_t iv = 2 * j + 1;
-                if (!wait_all(bar_full + 8 * (iv % RING), (uint32_t)((iv / RING) & 1))) { ok = false; break; }
+                if (!wait_all(bar_full + 8 * (j & 3), (uint32_t)((j >> 2) & 1))) { ok = false; break; }
                 uint8_t *vs = smem + SM::OFF_RING + (iv % RING) * SM::STAGE;
                 const int row_first = max(0, tok0 + 1 - t_base);
                 bool found = false;
