@@ -81,14 +81,16 @@ cudaError_t launch_rope_kv(const AttnShape &sh, const RopeLaunch &a, const RopeT
 struct PromptLaunch {
     const void *q, *k, *v;      // strides in elements
     void *out;
-    const int32_t *items;       // device [n_items][4]: pie_prompt_plan's list
+    const int32_t *items;       // device [n_items][4]: pie_prompt_plan's list; NULL: at most prompt_inline_items() of them, in items_host
+    const int32_t *items_host;
     int64_t q_stride, k_stride, v_stride, n_tokens, n_items;
     int32_t tile_tokens;        // tokens of a 128-row tile; an item is two tiles
     float scale;
     int32_t *status;
 };
 cudaError_t prompt_configure(int head_dim, int dtype);
-cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, cudaStream_t stream);
+int64_t prompt_inline_items();
+cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, int n_sms, cudaStream_t stream);
 
 // ---- eviction by accumulated attention weight ------------------------------------------------------------
 struct EvictLaunch {

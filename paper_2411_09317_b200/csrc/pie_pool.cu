@@ -136,6 +136,7 @@ struct pie_pool {
     bool prefill_ready = false;
     bool rope_ready = false, prompt_ready = false, evict_ready = false;
     pie::RopeTable rope{};       // rotary_dim 0: not set (pie_set_rope)
+    int32_t *prompt_items = nullptr;   // host: the items of a small call
     int attn_weights_grid = 0;   // 0: not configured yet
     int32_t *evict_scratch = nullptr;   // per kept token its row, per (sequence, KV head) the number of them
     int64_t evict_words = 0;
@@ -807,6 +808,7 @@ void destroy_pool(pie_pool *p) {
     cudaFree(p->scratch.part_ml);
     cudaFree(p->scratch.scores);
     cudaFree(p->evict_scratch);
+    delete[] p->prompt_items;
     for (int t = 0; t < 2; ++t) {
         cudaFree(p->scratch.part_o_more[t]);
         cudaFree(p->scratch.part_ml_more[t]);
@@ -2194,31 +2196,42 @@ int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const voi
         pool->prompt_ready = true;
     }
     cudaStream_t stream = pool->stream[PIE_Q_COMPUTE];
+    pie::PromptLaunch a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = out;
+    a.n_items = n_items;
+    a.tile_tokens = tile_tokens;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.n_tokens = n_tokens;
+    a.scale = scale;
+    a.status = pool->status_dev;
+    // the items travel with the launch where they fit, else through the list ring
+    const bool ring = n_items > pie::prompt_inline_items();
     int64_t off = 0;
-    st = list_alloc(pool, 4 * n_items, &off);
-    if (st != PIE_OK) return st;
-    st = pie_prompt_plan(offsets_host, n_seqs, 2 * tile_tokens, pool->list_host + off, n_items, &n_items);
-    if (st != PIE_OK) return st;   // (nothing is enqueued; the ring's piece is free again)
-    cudaError_t e = cudaMemcpyAsync(pool->list_dev + off, pool->list_host + off, (size_t)n_items * 16, cudaMemcpyHostToDevice, stream);
-    if (e == cudaSuccess) {
-        pie::PromptLaunch a{};
-        a.q = q;
-        a.k = k;
-        a.v = v;
-        a.out = out;
-        a.items = pool->list_dev + off;
-        a.n_items = n_items;
-        a.tile_tokens = tile_tokens;
-        a.q_stride = q_stride;
-        a.k_stride = k_stride;
-        a.v_stride = v_stride;
-        a.n_tokens = n_tokens;
-        a.scale = scale;
-        a.status = pool->status_dev;
-        e = pie::launch_prompt_attention(pool_shape(pool), a, stream);
+    int32_t *host = pool->prompt_items;
+    if (ring) {
+        st = list_alloc(pool, 4 * n_items, &off);
+        if (st != PIE_OK) return st;
+        host = pool->list_host + off;
+    } else if (!host) {
+        host = pool->prompt_items = new (std::nothrow) int32_t[4 * pie::prompt_inline_items()];
+        if (!host) return PIE_ERR_NOMEM;
     }
+    st = pie_prompt_plan(offsets_host, n_seqs, 2 * tile_tokens, host, n_items, &n_items);
+    if (st != PIE_OK) return st;   // (nothing is enqueued; the ring's piece is free again)
+    a.items_host = host;
+    cudaError_t e = cudaSuccess;
+    if (ring) {
+        a.items = pool->list_dev + off;
+        e = cudaMemcpyAsync(pool->list_dev + off, host, (size_t)n_items * 16, cudaMemcpyHostToDevice, stream);
+    }
+    if (e == cudaSuccess) e = pie::launch_prompt_attention(pool_shape(pool), a, pool->n_sms, stream);
     st = end_layer_work(pool, e, 0);
-    if (st == PIE_OK) {
+    if (st == PIE_OK && ring) {
         st = list_commit(pool, off, 4 * n_items, stream);
         if (st != PIE_OK) pool->sticky = st;
     }

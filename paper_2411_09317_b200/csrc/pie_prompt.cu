@@ -20,6 +20,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <cstring>
 
 #include "../../include/pie.h"
 #include "pie_kernels.h"
@@ -36,23 +37,24 @@ constexpr int PR_THREADS = PR_SOFTMAX_THREADS + 128;  // + the issuing warp (8),
 // the third gives up: 2 x 128 x 208 + 128 x 88 = 384 x 168.
 constexpr int PR_REGS_SOFTMAX = 208, PR_REGS_REST = 88;
 static_assert(2 * PR_REGS_SOFTMAX + PR_REGS_REST == 3 * 168, "what one side takes the other gives");
-#ifndef PR_POLY
-#define PR_POLY 2
-#endif
 constexpr int PR_TMEM_COLS = 512;             // S0, S1 (128 each; P over them), O0, O1 (128 each)
 // A row's running maximum is raised - and its O and sum rescaled - only when a stage exceeds it by more than this (log2
 // units): probabilities are then at most 2^8, harmless in fp32 sums and in both 16-bit types, and after the first stages
 // hardly any stage rescales.
 constexpr float PR_LAZY = 8.f;
 
+constexpr int PR_INLINE = 192;   // items that travel with the launch's parameters: no copy in front of a small call
+
 struct PromptParams {
-    const int4 *items;       // {first token of the sequence, first token of the item (within it), sequence length, -}
+    const int4 *items;       // {first token of the sequence, first token of the item (within it), sequence length, -}; NULL: inline
     uint16_t *out;
     const uint16_t *v;       // (the values again, for the rare repair below)
     int32_t *status;
     int64_t v_stride;
     int32_t n_q_heads, n_kv_heads, group, tile_tokens;
+    int32_t n_work;          // items * KV heads
     float scale_log2e;
+    int4 inline_items[PR_INLINE];
 };
 
 template <int D>
@@ -62,8 +64,8 @@ struct PrSmem {
     static constexpr int RING = D == 128 ? 5 : 8;
     static constexpr int OFF_Q = 0;
     static constexpr int OFF_RING = OFF_Q + Q_BYTES;
-    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], s[2 tiles][2 parities], p[2], done[2], q
-    static constexpr int OFF_MISC = OFF_BAR + 16 * 8;         // [0] TMEM base, [1] abort, [2] a value was not finite
+    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], free[4], s[2], p[2], done[2], q[2], k0
+    static constexpr int OFF_MISC = OFF_BAR + 18 * 8;         // [0] TMEM base, [1] abort, [4 .. 7] items in which a value was not finite
     static constexpr int BYTES = OFF_MISC + 32;
 };
 
@@ -163,6 +165,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     using SM = PrSmem<D>;
     constexpr int HALVES = D / 64;
     constexpr int RING = SM::RING;
+    // Share of the exponentials, in eighths, that the arithmetic pipes take over from the special-function unit (16 a clock and SM,
+    // as many as the tensor core asks for with heads of 128).  More of them costs more instructions and more power than the unit's
+    // relief gives back: 10007 tokens, 32 heads: 0, 1, 2 eighths 702, 702, 731 us with heads of 128, 643, 634, 613 us with 64.
+    constexpr int POLY = D == 128 ? 1 : 2;
     extern __shared__ __align__(1024) uint8_t pr_smem[];
     uint8_t *smem = pr_smem;
     const uint32_t base = pf_smem_u32(pr_smem);
@@ -171,36 +177,50 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (tid == 0) pf_raise(p.status, STATUS_WAIT_TIMEOUT);
         return;
     }
-    // Full barriers: one for Q and K(0), then one for every V(j) with K(j + 1), four in turn.  There are no empty barriers: what
-    // a ring entry held has been used when the scores of a later stage are complete (MMAs of one thread complete in order), so the
-    // loading warp waits for those.  It may be a stage behind the softmax warps, hence the scores' barriers by stage parity (a
-    // parity wait may be at most one phase behind).
-    const uint32_t bar_full = base + SM::OFF_BAR, bar_s = bar_full + 32, bar_p = bar_s + 32, bar_done = bar_p + 16, bar_q = bar_done + 16;
-    auto bar_scores = [&](int t, int32_t j) { return bar_s + 16 * t + 8 * (j & 1); };
+    // A CTA works through its items without a break: the stages of all of them form one sequence g = 0, 1, ...  Ring entry 2 g
+    // is K, 2 g + 1 is V of stage g.  full[g & 3]: V(g) and K(g + 1) have landed.  free[f & 3]: f = 0: the first scores, f = g + 1:
+    // all MMAs of stage g (O += P V of both tiles and the next scores) are complete.  Per tile: s: scores complete, p: P in place,
+    // done: O of the item complete, q: its query rows have landed.
+    const uint32_t bar_full = base + SM::OFF_BAR, bar_free = bar_full + 32, bar_s = bar_free + 32, bar_p = bar_s + 16, bar_done = bar_p + 16;
+    const uint32_t bar_q = bar_done + 16, bar_k0 = bar_q + 16;
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
 
-    // ---- which rows
-    const int32_t item = blockIdx.x / p.n_kv_heads, kvh = blockIdx.x - item * p.n_kv_heads;
-    const int4 it = __ldg(p.items + item);
-    const int32_t seq0 = it.x, tok0 = it.y, len = it.z;
+    // ---- the CTA's items: the list goes from long to short, and every other pass over the CTAs runs backwards, so that all get
+    // about the same number of stages (every warp works the sequence out for itself)
     const int32_t G = p.group, TT = p.tile_tokens;
-    // stages of each tile: what its last token sees (a tile behind the sequence's end has none)
-    const int32_t end0 = min(tok0 + TT, len), end1 = min(tok0 + 2 * TT, len);
-    const int32_t n0 = (end0 + PR_KV - 1) / PR_KV, n1 = end1 > end0 ? (end1 + PR_KV - 1) / PR_KV : 0;
-    const int32_t n_stages = max(n0, n1);
+    struct Item {
+        int32_t kvh, seq0, tok0, len, n0, n1, n;   // n0, n1: stages of each tile - what its last token sees (0: no such tile); n: the larger
+    };
+    auto get_item = [&](int32_t k, Item &it) {     // the CTA's k-th; false: there are no more
+        const int32_t x = (k & 1) ? (k + 1) * (int32_t)gridDim.x - 1 - (int32_t)blockIdx.x : k * (int32_t)gridDim.x + (int32_t)blockIdx.x;
+        if (x >= p.n_work) return false;
+        const int32_t i = x / p.n_kv_heads;
+        const int4 v = p.items != nullptr ? __ldg(p.items + i) : p.inline_items[i];
+        it.kvh = x - i * p.n_kv_heads;
+        it.seq0 = v.x;
+        it.tok0 = v.y;
+        it.len = v.z;
+        const int32_t end0 = min(it.tok0 + TT, it.len), end1 = min(it.tok0 + 2 * TT, it.len);
+        it.n0 = (end0 + PR_KV - 1) / PR_KV;
+        it.n1 = end1 > end0 ? (end1 + PR_KV - 1) / PR_KV : 0;
+        it.n = max(it.n0, it.n1);
+        return true;
+    };
 
     if (tid == 0) {
         for (int i = 0; i < 4; ++i) {
             pf_mbar_init(bar_full + 8 * i, 1);
-            pf_mbar_init(bar_s + 8 * i, 1);
+            pf_mbar_init(bar_free + 8 * i, 1);
+            misc[4 + i] = 0;
         }
-        pf_mbar_init(bar_q, 1);
+        pf_mbar_init(bar_k0, 1);
         for (int t = 0; t < 2; ++t) {
+            pf_mbar_init(bar_q + 8 * t, 1);
+            pf_mbar_init(bar_s + 8 * t, 1);
             pf_mbar_init(bar_p + 8 * t, 128);
             pf_mbar_init(bar_done + 8 * t, 1);
         }
         misc[1] = 0;
-        misc[2] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -241,40 +261,72 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_REST));
     if (warp == 9) {
         // =============================================================================== the loading warp
-        // Ring entry i (slot i % RING) holds K (even i) or V (odd i) of stage i / 2.
-        auto load = [&](int32_t i, uint32_t bar) {
-            const uint32_t dst = base + SM::OFF_RING + (uint32_t)(i % RING) * SM::STAGE;
-            for (int h = 0; h < HALVES; ++h)
-                pr_tma_3d(dst + h * (PR_KV * 128), (i & 1) ? &map_v : &map_k, 64 * h, kvh, seq0 + (i >> 1) * PR_KV, bar);
+        int32_t freed = -1;   // free[] waited for so far
+        auto need = [&](int32_t f) {
+            for (; freed < f; ++freed)
+                if (!wait_all(bar_free + 8 * ((freed + 1) & 3), (uint32_t)(((freed + 1) >> 2) & 1))) return false;
+            return true;
         };
-        const int last = n1 > 0 ? 1 : 0;
-        if (lane == 0) {
-            const uint32_t q_rows = (uint32_t)(G * TT);
-            pf_mbar_expect_tx(bar_q, (last + 1) * q_rows * D * 2 + SM::STAGE);
-            for (int t = 0; t <= last; ++t)
-                for (int h = 0; h < HALVES; ++h)
-                    pr_tma_3d(base + SM::OFF_Q + t * (TC_M * D * 2) + h * (TC_M * 128), &map_q, 64 * h, kvh * G, seq0 + tok0 + t * TT, bar_q);
-            load(0, bar_q);
-        }
-        __syncwarp();
-        int32_t issued = 0;
-        for (int32_t j = 0; j < n_stages; ++j) {   // V(j) and K(j + 1)
-            // the slots' entries before: 2 j + 1 - RING and 2 j + 2 - RING, of which the newer was used by the scores of this stage
-            // (a K) or by an O += P V that they follow (a V)
-            const int32_t used = (2 * j + 3 - RING) / 2;
-            if (2 * j + 2 >= RING && !wait_all(bar_scores(last, used), (uint32_t)((used >> 1) & 1))) break;
-            if (lane == 0) {
-                const uint32_t bar = bar_full + 8 * (j & 3);
-                pf_mbar_expect_tx(bar, j + 1 < n_stages ? 2 * SM::STAGE : SM::STAGE);
-                load(2 * j + 1, bar);
-                if (j + 1 < n_stages) load(2 * j + 2, bar);
-            }
+        auto load_q = [&](const Item &it) {
+            if (lane == 0)
+                for (int t = 0; t < (it.n1 > 0 ? 2 : 1); ++t) {
+                    pf_mbar_expect_tx(bar_q + 8 * t, (uint32_t)(G * TT) * D * 2);
+                    for (int h = 0; h < HALVES; ++h)
+                        pr_tma_3d(base + SM::OFF_Q + t * (TC_M * D * 2) + h * (TC_M * 128), &map_q, 64 * h, it.kvh * G, it.seq0 + it.tok0 + t * TT, bar_q + 8 * t);
+                }
             __syncwarp();
-            issued = j + 1;
+        };
+        auto load_kv = [&](const CUtensorMap *map, const Item &it, int32_t j, uint32_t slot, uint32_t bar) {
+            if (lane == 0)
+                for (int h = 0; h < HALVES; ++h)
+                    pr_tma_3d(base + SM::OFF_RING + slot * SM::STAGE + h * (PR_KV * 128), map, 64 * h, it.kvh, it.seq0 + j * PR_KV, bar);
+            __syncwarp();
+        };
+        Item it, next;
+        bool more = get_item(0, it), ok = true;
+        int32_t g = 0, q_count[2] = {0, 0};
+        uint32_t slot = 1;
+        if (more) {
+            if (lane == 0) pf_mbar_expect_tx(bar_k0, SM::STAGE);
+            __syncwarp();
+            load_q(it);
+            load_kv(&map_k, it, 0, 0, bar_k0);
+            q_count[0] = 1;
+            q_count[1] = it.n1 > 0;
         }
-        if (dead()) {   // giving up: wait (bounded) for the copies that still write into this CTA's shared memory
-            pf_mbar_wait(bar_q, 0);
-            for (int32_t j = max(0, issued - 4); j < issued; ++j) pf_mbar_wait(bar_full + 8 * (j & 3), (uint32_t)((j >> 2) & 1));
+        for (int32_t k = 0; more && ok; ++k) {
+            more = get_item(k + 1, next);
+            for (int32_t j = 0; j < it.n && ok; ++j, ++g) {
+                const bool last = j + 1 == it.n;
+                const uint32_t bar = bar_full + 8 * (g & 3);
+                // the slot of V(g) held K(g - 2), used in stage g - 3 (ring of 5; of 8: V(g - 4)); that of K(g + 1) held V(g - 2) (of 8: K(g - 3))
+                ok = need(RING == 5 ? g - 2 : g - 3);
+                if (!ok) break;
+                if (lane == 0) pf_mbar_expect_tx(bar, last && !more ? SM::STAGE : 2 * SM::STAGE);
+                __syncwarp();
+                load_kv(&map_v, it, j, slot, bar);
+                slot = slot + 1 == RING ? 0 : slot + 1;
+                if (!last || more) {
+                    if (need(RING == 5 ? g - 1 : g - 3)) load_kv(&map_k, last ? next : it, last ? 0 : j + 1, slot, bar);
+                    else ok = false;
+                }
+                slot = slot + 1 == RING ? 0 : slot + 1;
+                if (last && more && ok) {   // the item's last scores are complete: its query rows make room
+                    ok = need(g);
+                    if (ok) {
+                        load_q(next);
+                        q_count[0] += 1;
+                        q_count[1] += next.n1 > 0;
+                    }
+                }
+            }
+            it = next;
+        }
+        if (!ok || dead()) {   // giving up: wait (bounded) for the copies that still write into this CTA's shared memory
+            for (int t = 0; t < 2; ++t)
+                if (q_count[t] > 0) pf_mbar_wait(bar_q + 8 * t, (uint32_t)((q_count[t] - 1) & 1));
+            if (q_count[0] > 0) pf_mbar_wait(bar_k0, 0);
+            for (int32_t i = max(0, g - 3); i <= g; ++i) pf_mbar_wait(bar_full + 8 * (i & 3), (uint32_t)((i >> 2) & 1));
         }
         __syncwarp();
     } else if (warp == 8) {
@@ -286,40 +338,65 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t leader = lane == 0 ? 1u : 0u;
         const uint64_t q_desc = smem_desc(base + SM::OFF_Q, 16, 1024), k_desc = smem_desc(base + SM::OFF_RING, 16, 1024);
         const uint64_t v_desc = smem_desc(base + SM::OFF_RING, PR_KV * 128, 1024);
-        // S of a tile and stage, K in ring slot `slot`
-        auto issue_s = [&](int t, int32_t j, uint32_t slot) {
+        // S of a tile, K in ring slot `slot`
+        auto issue_s = [&](int t, uint32_t slot) {
             tc_fence_after();
             const uint64_t qd = q_desc + (uint64_t)(t * (TC_M * D * 2) >> 4), kd = k_desc + (uint64_t)(slot * (SM::STAGE >> 4));
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
                 pr_mma_ss(leader, t * 128, qd + (uint64_t)(((ks >> 2) * (TC_M * 128) + (ks & 3) * 32) >> 4),
                           kd + (uint64_t)(((ks >> 2) * (PR_KV * 128) + (ks & 3) * 32) >> 4), IDESC_S, ks > 0 ? 1u : 0u);
-            pr_commit(leader, bar_scores(t, j));
+            pr_commit(leader, bar_s + 8 * t);
         };
-        bool ok = wait_all(bar_q, 0);
-        if (ok) {
-            issue_s(0, 0, 0);
-            if (n1 > 0) issue_s(1, 0, 0);
+        Item it, next;
+        bool more = get_item(0, it), ok = true;
+        uint32_t p_count[2] = {0, 0}, q_count[2] = {0, 0};
+        if (more) {
+            ok = wait_all(bar_k0, 0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                if (ok && (t == 0 || it.n1 > 0)) {
+                    ok = wait_all(bar_q + 8 * t, 0);
+                    q_count[t] = 1;
+                    if (ok) issue_s(t, 0);
+                }
+            pr_commit(leader, bar_free);
         }
         uint32_t v_slot = 1;
-        for (int32_t j = 0; ok && j < n_stages; ++j) {
-            const uint32_t k_slot = v_slot + 1 == RING ? 0 : v_slot + 1;
-            const uint64_t vd = v_desc + (uint64_t)(v_slot * (SM::STAGE >> 4));
-            ok = wait_all(bar_full + 8 * (j & 3), (uint32_t)((j >> 2) & 1));   // V(j) and K(j + 1) have landed
+        int32_t g = 0;
+        for (int32_t k = 0; more && ok; ++k) {
+            more = get_item(k + 1, next);
+            const int32_t nx0 = more ? next.n0 : 0, nx1 = more ? next.n1 : 0;
+            for (int32_t j = 0; ok && j < it.n; ++j, ++g) {
+                const uint32_t k_slot = v_slot + 1 == RING ? 0 : v_slot + 1;
+                const uint64_t vd = v_desc + (uint64_t)(v_slot * (SM::STAGE >> 4));
+                const bool last = j + 1 == it.n;
+                ok = wait_all(bar_full + 8 * (g & 3), (uint32_t)((g >> 2) & 1));   // V(g) and K(g + 1) have landed
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int32_t n = t == 0 ? n0 : n1;
-                if (!ok || j >= n) continue;
-                ok = wait_all(bar_p + 8 * t, (uint32_t)(j & 1));
-                if (!ok) continue;
-                tc_fence_after();
+                for (int t = 0; t < 2; ++t) {
+                    const int32_t n = t == 0 ? it.n0 : it.n1, nx = t == 0 ? nx0 : nx1;
+                    if (ok && j < n) {
+                        ok = wait_all(bar_p + 8 * t, p_count[t] & 1u);
+                        ++p_count[t];
+                        if (!ok) continue;
+                        tc_fence_after();
 #pragma unroll
-                for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
-                    pr_mma_ts(leader, 256 + t * 128, t * 128 + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), IDESC_O, (j > 0 || ks > 0) ? 1u : 0u);
-                if (j + 1 == n) pr_commit(leader, bar_done + 8 * t);
-                else issue_s(t, j + 1, k_slot);
+                        for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
+                            pr_mma_ts(leader, 256 + t * 128, t * 128 + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), IDESC_O, (j > 0 || ks > 0) ? 1u : 0u);
+                        if (j + 1 == n) pr_commit(leader, bar_done + 8 * t);
+                    }
+                    if (ok && (j + 1 < n || (last && nx > 0))) {   // the item's next scores, or the next item's first
+                        if (j + 1 >= n) {
+                            ok = wait_all(bar_q + 8 * t, q_count[t] & 1u);
+                            ++q_count[t];
+                        }
+                        if (ok) issue_s(t, k_slot);
+                    }
+                }
+                pr_commit(leader, bar_free + 8 * ((g + 1) & 3));
+                v_slot = k_slot + 1 == RING ? 0 : k_slot + 1;
             }
-            v_slot = k_slot + 1 == RING ? 0 : k_slot + 1;
+            it = next;
         }
         __syncwarp();
     }
@@ -328,18 +405,26 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PR_REGS_SOFTMAX));
         const int t = warp >> 2;
         const int r = tid & 127;                                      // row of the tile
-        const int32_t n = t == 0 ? n0 : n1;
         const int32_t my_tok = r / G, my_g = r - my_tok * G;
+        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tmem_s = t * 128 + lane_addr, tmem_o = 256 + t * 128 + lane_addr;
+        Item it, next;
+        bool more = get_item(0, it), ok = true;
+        uint32_t s_count = 0, done_count = 0;
+        int32_t g0 = 0;   // the item's first stage
+        for (int32_t k = 0; more && ok; ++k, g0 += it.n, it = next) {
+        more = get_item(k + 1, next);
+        const int32_t n = t == 0 ? it.n0 : it.n1, tok0 = it.tok0;
+        if (n == 0) continue;
         const int32_t first = tok0 + t * TT;                          // the tile's first position
         const int32_t my_pos = first + my_tok;
-        const bool row_valid = my_tok < TT && my_pos < len;
-        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tmem_s = tmem + t * 128 + lane_addr, tmem_o = tmem + 256 + t * 128 + lane_addr;
+        const bool row_valid = my_tok < TT && my_pos < it.len;
+        volatile uint32_t *not_finite = misc + 4 + (k & 3);
         float m_run = -INFINITY, l_run = 0.f;
         bool spoiled = false;                                         // a score the row sees is NaN or +inf: so is the softmax
-        bool ok = true;
         for (int32_t j = 0; j < n; ++j) {
-            if (!wait_all(bar_scores(t, j), (uint32_t)((j >> 1) & 1))) { ok = false; break; }
+            if (!wait_all(bar_s + 8 * t, s_count & 1u)) { ok = false; break; }
+            ++s_count;
             tc_fence_after();
             uint32_t sv[4][32];
 #pragma unroll
@@ -382,7 +467,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (int w = 0; w < 32; ++w) {
                     const int c = 64 * h + 2 * w;
                     const float2 x = pr_fma2(make_float2(__uint_as_float(sv[c >> 5][c & 31]), __uint_as_float(sv[c >> 5][(c & 31) + 1])), sc2, nm2);
-                    const float2 e = (w & 7) < PR_POLY ? pr_exp2_poly(x) : make_float2(pf_exp2(x.x), pf_exp2(x.y));
+                    const float2 e = (w & 7) < POLY ? pr_exp2_poly(x) : make_float2(pf_exp2(x.x), pf_exp2(x.y));
                     if (w & 1) s1 = pr_add2(s1, e);
                     else s0 = pr_add2(s0, e);
                     pw[w] = pf_pack2<BF16>(e.x, e.y);
@@ -406,9 +491,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (masked) {
                 // Values that some row of the item may not see meet P = 0 there, which hides everything but NaN and infinities.
                 // Those are cleared in the stage and, if there were any, added at the end to the rows that do see them.
-                const int32_t iv = 2 * j + 1;
-                if (!wait_all(bar_full + 8 * (j & 3), (uint32_t)((j >> 2) & 1))) { ok = false; break; }
-                uint8_t *vs = smem + SM::OFF_RING + (iv % RING) * SM::STAGE;
+                const int32_t g = g0 + j;
+                if (!wait_all(bar_full + 8 * (g & 3), (uint32_t)((g >> 2) & 1))) { ok = false; break; }
+                uint8_t *vs = smem + SM::OFF_RING + (2 * g + 1) % RING * SM::STAGE;
                 const int row_first = max(0, tok0 + 1 - t_base);
                 bool found = false;
                 for (int e = row_first * 8 + r; e < PR_KV * 8; e += 128)
@@ -425,22 +510,23 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             *at = w;
                         }
                     }
-                if (found) misc[2] = 1;
+                if (found) *not_finite = (uint32_t)k + 1u;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
             tmem_wait_st();
             tc_fence_before();
             pf_mbar_arrive(bar_p + 8 * t);
         }
-        if (ok && n > 0) ok = wait_all(bar_done + 8 * t, 0u);
+        if (ok) ok = wait_all(bar_done + 8 * t, done_count & 1u);
+        ++done_count;
         // ---- out = O / l, rounded to the 16-bit type (nearest even).  The TMEM loads are warp-wide: rows beyond the tile take
         // part in them and store nothing.
-        if (ok && n > 0) {
+        if (ok) {
             tc_fence_after();
             const float inv = spoiled ? __int_as_float(0x7fc00000) : 1.f / l_run;
-            const bool repair = misc[2] != 0;
-            uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((int64_t)(seq0 + my_pos) * p.n_q_heads + kvh * G + my_g) * D);
-            const uint16_t *vrow = p.v + (int64_t)(seq0 + tok0 + 1) * p.v_stride + (int64_t)kvh * D;
+            const bool repair = *not_finite == (uint32_t)k + 1u;
+            uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((int64_t)(it.seq0 + my_pos) * p.n_q_heads + it.kvh * G + my_g) * D);
+            const uint16_t *vrow = p.v + (int64_t)(it.seq0 + tok0 + 1) * p.v_stride + (int64_t)it.kvh * D;
 #pragma unroll 1
             for (int c0 = 0; c0 < D; c0 += 32) {
                 uint32_t ov[32];
@@ -467,6 +553,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                 }
             }
+        }
         }
     }
     tc_fence_before();
@@ -515,7 +602,9 @@ cudaError_t prompt_configure(int head_dim, int dtype) {
     });
 }
 
-cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, cudaStream_t stream) {
+int64_t prompt_inline_items() { return PR_INLINE; }
+
+cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, int n_sms, cudaStream_t stream) {
     if (a.n_items <= 0) return cudaSuccess;
     const int group = sh.n_q_heads / sh.n_kv_heads;
     CUtensorMap map_q, map_k, map_v;
@@ -525,6 +614,8 @@ cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, 
     if (e != cudaSuccess) return e;
     PromptParams p;
     p.items = reinterpret_cast<const int4 *>(a.items);
+    if (a.items == nullptr) std::memcpy(p.inline_items, a.items_host, (size_t)a.n_items * 16);
+    p.n_work = (int32_t)(a.n_items * sh.n_kv_heads);
     p.out = (uint16_t *)a.out;
     p.v = (const uint16_t *)a.v;
     p.status = a.status;
@@ -535,7 +626,7 @@ cudaError_t launch_prompt_attention(const AttnShape &sh, const PromptLaunch &a, 
     p.tile_tokens = a.tile_tokens;
     p.scale_log2e = a.scale * 1.4426950408889634f;
     return dispatch_prompt(sh.head_dim, sh.dtype, [&](auto kernel, int smem) {
-        kernel<<<(unsigned)(a.n_items * sh.n_kv_heads), PR_THREADS, smem, stream>>>(map_q, map_k, map_v, p);
+        kernel<<<(unsigned)std::min<int64_t>(p.n_work, n_sms), PR_THREADS, smem, stream>>>(map_q, map_k, map_v, p);
         return cudaGetLastError();
     });
 }
