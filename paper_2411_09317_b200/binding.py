@@ -248,17 +248,15 @@ def pie_rope_plan(head_dim, rotary_dim, pair_axis, inv_freq):
 def pie_rope_kv_write(pool, layer, q, q_out, k, k_out, v, positions_dev, token_seq_dev, token_pos_dev, n_tokens, block_table_dev,
                       max_blocks_per_seq, n_seqs, q_stride=0, k_stride=0, v_stride=0) -> None:
     """Device pointers (0 / None for NULL); strides in elements from a token to the next, 0 for dense rows."""
-    check(lib.pie_rope_kv_write(pool, layer, _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), _ptr(v), _ptr(positions_dev),
-                                _ptr(token_seq_dev), _ptr(token_pos_dev), n_tokens, _ptr(block_table_dev), max_blocks_per_seq, n_seqs,
-                                q_stride, k_stride, v_stride), "pie_rope_kv_write")
+    check(lib.pie_rope_kv_write(pool, layer, q, q_out, k, k_out, v, positions_dev, token_seq_dev, token_pos_dev, n_tokens,
+                                block_table_dev, max_blocks_per_seq, n_seqs, q_stride, k_stride, v_stride), "pie_rope_kv_write")
 
 
 def pie_prompt_attention(pool, q, k, v, out, offsets_host, n_seqs, scale, q_stride=0, k_stride=0, v_stride=0) -> None:
     """q / k / v / out: device pointers; offsets_host [n_seqs + 1]: numpy int32; strides in elements, 0 for dense rows."""
     off = _np_i32(offsets_host)
     assert len(off) > n_seqs
-    check(lib.pie_prompt_attention(pool, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(off), n_seqs, scale, q_stride, k_stride, v_stride),
-          "pie_prompt_attention")
+    check(lib.pie_prompt_attention(pool, q, k, v, out, _ptr(off), n_seqs, scale, q_stride, k_stride, v_stride), "pie_prompt_attention")
 
 
 def pie_prompt_plan(offsets, item_tokens) -> np.ndarray:
@@ -275,18 +273,16 @@ def pie_decode_attention_weights(pool, layer, q, out, block_table_dev, max_block
     """weights: device fp32 [n_seqs][n_kv_heads][weights_stride], added to."""
     bth = None if block_table_host is None else _np_i32(block_table_host)
     clh = None if ctx_lens_host is None else _np_i32(ctx_lens_host)
-    check(lib.pie_decode_attention_weights(pool, layer, _ptr(q), _ptr(out), _ptr(block_table_dev), max_blocks_per_seq, _ptr(ctx_lens_dev),
-                                           _ptr(bth), _ptr(clh), n_seqs, scale, _ptr(k_new), _ptr(v_new), _ptr(weights), weights_stride),
-          "pie_decode_attention_weights")
+    check(lib.pie_decode_attention_weights(pool, layer, q, out, block_table_dev, max_blocks_per_seq, ctx_lens_dev, _ptr(bth), _ptr(clh),
+                                           n_seqs, scale, k_new, v_new, weights, weights_stride), "pie_decode_attention_weights")
 
 
 def pie_kv_evict(pool, layer, block_table_dev, max_blocks_per_seq, ctx_lens_dev, n_seqs, weights, weights_stride, budget, recent,
                  dst_block_table_dev=None, dst_max_blocks=0, weights_out=None, weights_out_stride=0, new_lens_dev=None,
                  kept_dev=None) -> None:
     """Device pointers; without dst_block_table_dev / weights_out the keys, values / weights are moved in place."""
-    check(lib.pie_kv_evict(pool, layer, _ptr(block_table_dev), max_blocks_per_seq, _ptr(ctx_lens_dev), n_seqs, _ptr(weights), weights_stride,
-                           budget, recent, _ptr(dst_block_table_dev), dst_max_blocks, _ptr(weights_out), weights_out_stride,
-                           _ptr(new_lens_dev), _ptr(kept_dev)), "pie_kv_evict")
+    check(lib.pie_kv_evict(pool, layer, block_table_dev, max_blocks_per_seq, ctx_lens_dev, n_seqs, weights, weights_stride, budget, recent,
+                           dst_block_table_dev, dst_max_blocks, weights_out, weights_out_stride, new_lens_dev, kept_dev), "pie_kv_evict")
 
 
 def pie_set_violation_trigger(pool, share) -> None:

@@ -74,7 +74,7 @@ struct RopeLaunch {
     float k_scale, v_scale;
     int32_t *status;
 };
-cudaError_t rope_configure();
+cudaError_t rope_configure(const AttnShape &sh);
 cudaError_t launch_rope_kv(const AttnShape &sh, const RopeLaunch &a, const RopeTable &table, int n_sms, cudaStream_t stream);
 
 // ---- attention over whole prompts ---------------------------------------------------------------------
@@ -107,7 +107,8 @@ struct EvictLaunch {
     int32_t *status;
 };
 cudaError_t evict_configure();
-cudaError_t launch_evict(const AttnShape &sh, const EvictLaunch &a, int n_sms, cudaStream_t stream);
+int64_t evict_chunks(const EvictLaunch &a);
+cudaError_t launch_evict(const AttnShape &sh, const EvictLaunch &a, cudaStream_t stream);
 
 struct AttnScratch {
     int32_t *chunk_off;  // [max_seqs + 1] (used only for batches beyond the in-kernel plan)

@@ -2129,7 +2129,7 @@ int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out,
     if (st != PIE_OK) return st;
     if (n_tokens == 0) return PIE_OK;
     if (!pool->rope_ready) {
-        PIE_CUDA(pie::rope_configure());
+        PIE_CUDA(pie::rope_configure(pool_shape(pool)));
         pool->rope_ready = true;
     }
     cudaStream_t stream = pool->stream[PIE_Q_COMPUTE];
@@ -2281,7 +2281,25 @@ int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, 
         return PIE_ERR_INVALID;
     }
     const int64_t pairs = (int64_t)n_seqs * pool->cfg.n_kv_heads;
-    if (pairs > 0x7fffffffll) return PIE_ERR_INVALID;
+    pie::EvictLaunch a{};
+    a.block_table = block_table_dev;
+    a.ctx_lens = ctx_lens_dev;
+    a.dst_table = dst_block_table_dev;
+    a.slot_table = pool->slot_table_dev + (int64_t)layer * pool->cfg.n_logical_blocks;
+    a.weights = weights;
+    a.weights_out = weights_out;
+    a.weights_stride = weights_stride;
+    a.weights_out_stride = weights_out_stride;
+    a.new_lens = new_lens_dev;
+    a.kept = kept_dev;
+    a.gpu_pool = pool->gpu_base;
+    a.max_blocks = max_blocks_per_seq;
+    a.dst_max_blocks = dst_max_blocks;
+    a.n_seqs = n_seqs;
+    a.budget = budget;
+    a.recent = recent;
+    a.status = pool->status_dev;
+    if (pairs * std::max<int64_t>(1, pie::evict_chunks(a)) > 0x7fffffffll) return PIE_ERR_INVALID;
     OnDevice on(pool->device);
     if (capturing(pool)) return PIE_ERR_UNSUPPORTED;
     int st = poll(pool);
@@ -2308,30 +2326,12 @@ int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, 
         }
         pool->evict_words = words;
     }
+    a.counts = pool->evict_scratch;
+    a.rows = pool->evict_scratch + pairs;
     int64_t ticket = 0;
     st = begin_layer_work(pool, layer, true, &ticket);
     if (st != PIE_OK) return st;
-    pie::EvictLaunch a{};
-    a.block_table = block_table_dev;
-    a.ctx_lens = ctx_lens_dev;
-    a.dst_table = dst_block_table_dev;
-    a.slot_table = pool->slot_table_dev + (int64_t)layer * pool->cfg.n_logical_blocks;
-    a.weights = weights;
-    a.weights_out = weights_out;
-    a.weights_stride = weights_stride;
-    a.weights_out_stride = weights_out_stride;
-    a.new_lens = new_lens_dev;
-    a.kept = kept_dev;
-    a.counts = pool->evict_scratch;
-    a.rows = pool->evict_scratch + pairs;
-    a.gpu_pool = pool->gpu_base;
-    a.max_blocks = max_blocks_per_seq;
-    a.dst_max_blocks = dst_max_blocks;
-    a.n_seqs = n_seqs;
-    a.budget = budget;
-    a.recent = recent;
-    a.status = pool->status_dev;
-    return end_layer_work(pool, pie::launch_evict(pool_shape(pool), a, pool->n_sms, pool->stream[PIE_Q_COMPUTE]), ticket);
+    return end_layer_work(pool, pie::launch_evict(pool_shape(pool), a, pool->stream[PIE_Q_COMPUTE]), ticket);
 }
 
 int pie_report_throughput(pie_pool *pool, double throughput) {

@@ -5,15 +5,16 @@
 // product has no fraction left at 2^24 radians and is off by 0.06 at a million), and no range reduction is needed before
 // sincospif.
 //
-// The work is moving bytes: q, k and v are read once, q_out, k_out and the cache rows written once.  A CTA takes a few
-// consecutive tokens (and, where there are few tokens, a share of their heads).  It first puts the cosines and sines of
-// its tokens' pairs into shared memory - they are shared by all heads, and evaluating them per head would cost more
-// instructions than everything else - and then walks over (token, head, 16 elements): two 16-byte loads, which hold both
-// elements of eight pairs in either pair layout, and two 16-byte stores per destination.
+// The work is moving bytes: q, k and v are read once, q_out, k_out and the cache rows written once.  A CTA takes T consecutive
+// tokens.  It first puts the cosines and sines of its tokens' pairs into shared memory - all heads share them, and evaluating
+// them per head would cost more instructions than everything else.  Then a thread keeps one place of the head (16 elements, both
+// halves of eight pairs in either pair layout) of one token, with the pairs' factors in registers, and walks over heads: q, k and
+// v alike, two 16-byte loads and two 16-byte stores per destination each, three heads' loads in flight.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "../../include/pie.h"
 #include "pie_kernels.h"
@@ -23,7 +24,7 @@ namespace pie {
 namespace {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_MAX_TOKENS = 8;   // tokens of a CTA at most (shared memory: 8 x 64 pairs x 8 bytes)
+constexpr int ROPE_AHEAD = 3;        // heads whose loads are in flight
 
 struct RopeParams {
     RopeTable table;
@@ -34,8 +35,8 @@ struct RopeParams {
     int32_t *status;
     int64_t n_tokens, q_stride, k_stride, v_stride, n_gpu_slots;
     int32_t n_q_heads, n_kv_heads, head_dim, max_blocks, n_seqs, n_logical;
-    int32_t tokens_per_cta;
     float k_scale, v_scale;
+    float k_inv, v_inv;      // 1 / scale where that is exact (a power of two), else 0
 };
 
 template <bool BF16>
@@ -68,35 +69,40 @@ __device__ __forceinline__ uint4 rope_pack(const float (&x)[8]) {
     }
     return make_uint4(a[0], a[1], a[2], a[3]);
 }
-// eight values -> eight E4M3 bytes of value / scale: the append's rule (fp32 quotient, nearest even, saturating)
-__device__ __forceinline__ uint2 rope_pack8(const float (&x)[8], float scale) {
+// eight values -> eight E4M3 bytes of value / scale: the append's rule (fp32 quotient, nearest even, saturating).  The product
+// with the reciprocal of a power of two is that quotient; for other scales it would not always be.
+__device__ __forceinline__ uint2 rope_pack8(const float (&x)[8], float scale, float inv) {
     uint32_t b[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        const float lo = inv != 0.f ? x[2 * i] * inv : __fdiv_rn(x[2 * i], scale), hi = inv != 0.f ? x[2 * i + 1] * inv : __fdiv_rn(x[2 * i + 1], scale);
         uint16_t r;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(__fdiv_rn(x[2 * i + 1], scale)), "f"(__fdiv_rn(x[2 * i], scale)));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
         b[i] = r;
     }
     return make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
 }
 
-template <bool BF16, bool KV8>
+template <int D, int T, bool BF16, bool KV8>
 __global__ void __launch_bounds__(ROPE_THREADS)
 rope_kv_kernel(const __grid_constant__ RopeParams p) {
-    __shared__ float2 cs[ROPE_MAX_TOKENS][64];
-    __shared__ int32_t place[ROPE_MAX_TOKENS];   // slot * 16 + row of the token, -1: not written
+    constexpr int PLACES = D / 16, LANES = ROPE_THREADS / (PLACES * T);   // threads per head and token; heads side by side
+    __shared__ __align__(16) float2 cs[T][D / 2];
+    __shared__ int32_t place[T];   // slot * 16 + row of the token, -1: not written
     const int tid = threadIdx.x;
-    const int64_t t0 = (int64_t)blockIdx.x * p.tokens_per_cta;
-    const int nt = (int)min((int64_t)p.tokens_per_cta, p.n_tokens - t0);
+    const int64_t t0 = (int64_t)blockIdx.x * T;
+    const int nt = (int)min((int64_t)T, p.n_tokens - t0);
     const int pairs = p.table.rotary_dim >> 1;
 
-    for (int i = tid; i < nt * pairs; i += ROPE_THREADS) {
-        const int tt = i / pairs, pr = i - tt * pairs;
-        const int32_t pos = __ldg(p.positions + p.table.axis[pr] * p.n_tokens + t0 + tt);
-        const unsigned long long turn = (unsigned long long)(long long)pos * p.table.turns[pr];
-        float s, c;
-        sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
-        cs[tt][pr] = make_float2(c * p.table.amplitude, s * p.table.amplitude);
+    for (int i = tid; i < T * (D / 2); i += ROPE_THREADS) {
+        const int tt = i / (D / 2), pr = i % (D / 2);
+        if (tt < nt && pr < pairs) {
+            const int32_t pos = __ldg(p.positions + p.table.axis[pr] * p.n_tokens + t0 + tt);
+            const unsigned long long turn = (unsigned long long)(long long)pos * p.table.turns[pr];
+            float s, c;
+            sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
+            cs[tt][pr] = make_float2(c * p.table.amplitude, s * p.table.amplitude);
+        }
     }
     if (p.block_table != nullptr && tid >= ROPE_THREADS - 32 && (tid & 31) < nt) {
         const int tt = tid & 31;
@@ -112,94 +118,124 @@ rope_kv_kernel(const __grid_constant__ RopeParams p) {
         }
         place[tt] = at;
     }
-    __syncthreads();
 
-    const int D = p.head_dim, per_head = D >> 4, rot = p.table.rotary_dim >> 4;   // items of 16 elements: all, rotated ones
+    const int j = tid % PLACES, tt = tid / PLACES % T, lane = tid / (PLACES * T);
+    const int64_t t = t0 + tt;
+    const bool live = tt < nt;
     const int hq = p.q != nullptr ? p.n_q_heads : 0, hk = p.k != nullptr ? p.n_kv_heads : 0;
     const int hv = p.block_table != nullptr ? p.n_kv_heads : 0;
-    const int per_token = (hq + hk + hv) * per_head;
-    const int first = blockIdx.y * ROPE_THREADS + tid, step = gridDim.y * ROPE_THREADS;
-    for (int i = first; i < nt * per_token; i += step) {
-        const int tt = i / per_token, r = i - tt * per_token;
-        const int head = r / per_head, j = r - head * per_head;
-        const int64_t t = t0 + tt;
-        const bool is_q = head < hq, is_v = head >= hq + hk;
-        const int h = is_q ? head : is_v ? head - hq - hk : head - hq;
-        const uint16_t *src = is_q ? p.q + t * p.q_stride : is_v ? p.v + t * p.v_stride : p.k + t * p.k_stride;
-        // the item's two vectors of eight: both elements of eight pairs, or 16 elements behind the rotated ones
-        const bool turned = !is_v && j < rot;
-        const bool halves = turned && !p.table.adjacent;
-        const int va = halves ? j : 2 * j, vb = halves ? j + rot : 2 * j + 1;
-        const uint4 *row = reinterpret_cast<const uint4 *>(src + (int64_t)h * D);
-        uint4 wa = row[va], wb = row[vb];
-        float a[8], b[8];
-        if (turned || KV8) {
-            rope_unpack<BF16>(wa, a);
-            rope_unpack<BF16>(wb, b);
-        }
-        if (turned) {
-            const float4 *c4 = reinterpret_cast<const float4 *>(&cs[tt][8 * j]);
-            float2 c[8];
+    const int heads = live ? hq + hk + hv : 0;
+    const int rot = p.table.rotary_dim >> 4;
+    const bool turned = j < rot, adjacent = p.table.adjacent != 0;
+    // the two vectors of eight that a turned place consists of, and those of one that is passed through
+    const int ta = adjacent ? 2 * j : j, tb = adjacent ? 2 * j + 1 : j + rot;
+    auto load = [&](int head, uint4 &wa, uint4 &wb) {
+        const bool is_v = head >= hq + hk;
+        const uint16_t *src = head < hq ? p.q + t * p.q_stride + head * D : is_v ? p.v + t * p.v_stride + (head - hq - hk) * D : p.k + t * p.k_stride + (head - hq) * D;
+        const uint4 *row = reinterpret_cast<const uint4 *>(src);
+        const bool turn = turned && !is_v;
+        wa = row[turn ? ta : 2 * j];
+        wb = row[turn ? tb : 2 * j + 1];
+    };
+    uint4 wa[ROPE_AHEAD], wb[ROPE_AHEAD];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float4 f = c4[e];
-                c[2 * e] = make_float2(f.x, f.y);
-                c[2 * e + 1] = make_float2(f.z, f.w);
-            }
-            if (p.table.adjacent) {
+    for (int u = 0; u < ROPE_AHEAD; ++u)
+        if (lane + u * LANES < heads) load(lane + u * LANES, wa[u], wb[u]);   // (in flight while the factors are worked out)
+    __syncthreads();
+    float2 c[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x0 = a[2 * e], y0 = a[2 * e + 1], x1 = b[2 * e], y1 = b[2 * e + 1];
-                    a[2 * e] = x0 * c[e].x - y0 * c[e].y;
-                    a[2 * e + 1] = y0 * c[e].x + x0 * c[e].y;
-                    b[2 * e] = x1 * c[4 + e].x - y1 * c[4 + e].y;
-                    b[2 * e + 1] = y1 * c[4 + e].x + x1 * c[4 + e].y;
-                }
-            } else {
+    for (int e = 0; e < 8; ++e) c[e] = make_float2(1.f, 0.f);
+    if (turned && live) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = a[e], y = b[e];
-                    a[e] = x * c[e].x - y * c[e].y;
-                    b[e] = y * c[e].x + x * c[e].y;
-                }
-            }
-            wa = rope_pack<BF16>(a);
-            wb = rope_pack<BF16>(b);
-        }
-        if (is_q) {
-            uint4 *dst = reinterpret_cast<uint4 *>(p.q_out + (t * p.n_q_heads + h) * D);
-            dst[va] = wa;
-            dst[vb] = wb;
-            continue;
-        }
-        if (!is_v && p.k_out != nullptr) {
-            uint4 *dst = reinterpret_cast<uint4 *>(p.k_out + (t * p.n_kv_heads + h) * D);
-            dst[va] = wa;
-            dst[vb] = wb;
-        }
-        if (hv == 0 || place[tt] < 0) continue;
-        const int32_t slot = place[tt] >> 4, tr = place[tt] & 15;
-        const int64_t cache_row = (((int64_t)slot * p.n_kv_heads + h) * 2 + (is_v ? 1 : 0)) * 16 + tr;
-        if (KV8) {
-            const float sc = is_v ? p.v_scale : p.k_scale;
-            uint2 *dst = reinterpret_cast<uint2 *>(p.pool + cache_row * D);
-            dst[va] = rope_pack8(a, sc);
-            dst[vb] = rope_pack8(b, sc);
-        } else {
-            uint4 *dst = reinterpret_cast<uint4 *>(p.pool + cache_row * D * 2);
-            dst[va] = wa;
-            dst[vb] = wb;
+        for (int e = 0; e < 4; ++e) {
+            const float4 f = reinterpret_cast<const float4 *>(&cs[tt][8 * j])[e];
+            c[2 * e] = make_float2(f.x, f.y);
+            c[2 * e + 1] = make_float2(f.z, f.w);
         }
     }
+    const int32_t at = hv != 0 && live ? place[tt] : -1;
+    for (int h0 = lane; h0 < heads; h0 += ROPE_AHEAD * LANES) {
+#pragma unroll
+        for (int u = 0; u < ROPE_AHEAD; ++u) {
+            const int head = h0 + u * LANES;
+            if (head >= heads) break;
+            const bool is_q = head < hq, is_v = head >= hq + hk, turn = turned && !is_v;
+            const int h = is_q ? head : is_v ? head - hq - hk : head - hq;
+            const int va = turn ? ta : 2 * j, vb = turn ? tb : 2 * j + 1;
+            float a[8], b[8];
+            if (turn || (KV8 && !is_q)) {
+                rope_unpack<BF16>(wa[u], a);
+                rope_unpack<BF16>(wb[u], b);
+            }
+            if (turn) {
+                if (adjacent) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x0 = a[2 * e], y0 = a[2 * e + 1], x1 = b[2 * e], y1 = b[2 * e + 1];
+                        a[2 * e] = x0 * c[e].x - y0 * c[e].y;
+                        a[2 * e + 1] = y0 * c[e].x + x0 * c[e].y;
+                        b[2 * e] = x1 * c[4 + e].x - y1 * c[4 + e].y;
+                        b[2 * e + 1] = y1 * c[4 + e].x + x1 * c[4 + e].y;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = a[e], y = b[e];
+                        a[e] = x * c[e].x - y * c[e].y;
+                        b[e] = y * c[e].x + x * c[e].y;
+                    }
+                }
+                wa[u] = rope_pack<BF16>(a);
+                wb[u] = rope_pack<BF16>(b);
+            }
+            if (!is_v && (is_q || p.k_out != nullptr)) {
+                uint4 *dst = reinterpret_cast<uint4 *>(is_q ? p.q_out + (t * p.n_q_heads + h) * D : p.k_out + (t * p.n_kv_heads + h) * D);
+                dst[va] = wa[u];
+                dst[vb] = wb[u];
+            }
+            if (!is_q && at >= 0) {
+                const int64_t cache_row = (((int64_t)(at >> 4) * p.n_kv_heads + h) * 2 + (is_v ? 1 : 0)) * 16 + (at & 15);
+                if (KV8) {
+                    const float sc = is_v ? p.v_scale : p.k_scale, inv = is_v ? p.v_inv : p.k_inv;
+                    uint2 *dst = reinterpret_cast<uint2 *>(p.pool + cache_row * D);
+                    dst[va] = rope_pack8(a, sc, inv);
+                    dst[vb] = rope_pack8(b, sc, inv);
+                } else {
+                    uint4 *dst = reinterpret_cast<uint4 *>(p.pool + cache_row * D * 2);
+                    dst[va] = wa[u];
+                    dst[vb] = wb[u];
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < ROPE_AHEAD; ++u)
+            if (h0 + (ROPE_AHEAD + u) * LANES < heads) load(h0 + (ROPE_AHEAD + u) * LANES, wa[u], wb[u]);
+    }
+}
+
+template <typename F>
+cudaError_t dispatch_rope(const AttnShape &sh, bool few, F &&f) {
+    // few tokens: one per CTA
+    auto by_type = [&](auto d, auto t) -> cudaError_t {
+        constexpr int D = decltype(d)::value, T = decltype(t)::value;
+        if (sh.kv_fp8) return sh.dtype == PIE_BF16 ? f(rope_kv_kernel<128, T, true, true>, T) : f(rope_kv_kernel<128, T, false, true>, T);
+        return sh.dtype == PIE_BF16 ? f(rope_kv_kernel<D, T, true, false>, T) : f(rope_kv_kernel<D, T, false, false>, T);
+    };
+    using C64 = std::integral_constant<int, 64>;
+    using C128 = std::integral_constant<int, 128>;
+    using One = std::integral_constant<int, 1>;
+    using Four = std::integral_constant<int, 4>;
+    if (sh.head_dim == 128) return few ? by_type(C128(), One()) : by_type(C128(), Four());
+    return few ? by_type(C64(), One()) : by_type(C64(), Four());
 }
 
 }  // namespace
 
-cudaError_t rope_configure() {
-    const void *fns[] = {(const void *)rope_kv_kernel<true, false>, (const void *)rope_kv_kernel<false, false>,
-                         (const void *)rope_kv_kernel<true, true>, (const void *)rope_kv_kernel<false, true>};
-    for (const void *f : fns) {
-        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+cudaError_t rope_configure(const AttnShape &sh) {
+    for (const bool few : {true, false}) {
+        const cudaError_t e = dispatch_rope(sh, few, [](auto kernel, int) {
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        });
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -234,22 +270,19 @@ cudaError_t launch_rope_kv(const AttnShape &sh, const RopeLaunch &a, const RopeT
     p.n_logical = sh.n_logical;
     p.k_scale = a.k_scale;
     p.v_scale = a.v_scale;
-    const int64_t items = (int64_t)(sh.n_q_heads + 2 * sh.n_kv_heads) * (sh.head_dim / 16);
-    p.tokens_per_cta = (int32_t)std::max<int64_t>(1, std::min<int64_t>(ROPE_MAX_TOKENS, a.n_tokens / (8 * n_sms)));
-    const int64_t gx = (a.n_tokens + p.tokens_per_cta - 1) / p.tokens_per_cta;
-    // few tokens: their heads are shared out among CTAs until there are about four per SM
-    const int64_t rounds = (items * p.tokens_per_cta + ROPE_THREADS - 1) / ROPE_THREADS;
-    const int64_t gy = std::max<int64_t>(1, std::min<int64_t>(rounds, 4 * n_sms / gx));
-    if (gx > 0x7fffffffll) return cudaErrorInvalidValue;
-    const dim3 grid((unsigned)gx, (unsigned)gy);
-    if (sh.kv_fp8) {
-        if (sh.dtype == PIE_BF16) rope_kv_kernel<true, true><<<grid, ROPE_THREADS, 0, stream>>>(p);
-        else rope_kv_kernel<false, true><<<grid, ROPE_THREADS, 0, stream>>>(p);
-    } else {
-        if (sh.dtype == PIE_BF16) rope_kv_kernel<true, false><<<grid, ROPE_THREADS, 0, stream>>>(p);
-        else rope_kv_kernel<false, false><<<grid, ROPE_THREADS, 0, stream>>>(p);
-    }
-    return cudaGetLastError();
+    auto exact_inverse = [](float x) {
+        int e = 0;
+        return std::frexp(x, &e) == 0.5f && e > -120 && e < 120 ? 1.f / x : 0.f;
+    };
+    p.k_inv = exact_inverse(a.k_scale);
+    p.v_inv = exact_inverse(a.v_scale);
+    // Four tokens per CTA once that still gives every SM several CTAs; below, one: a decode step's latency is what counts there
+    return dispatch_rope(sh, a.n_tokens < 16 * n_sms, [&](auto kernel, int tokens) {
+        const int64_t grid = (a.n_tokens + tokens - 1) / tokens;
+        if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
+        kernel<<<(unsigned)grid, ROPE_THREADS, 0, stream>>>(p);
+        return cudaGetLastError();
+    });
 }
 
 }  // namespace pie
