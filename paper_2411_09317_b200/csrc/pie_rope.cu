@@ -8,8 +8,9 @@
 // The work is moving bytes: q, k and v are read once, q_out, k_out and the cache rows written once.  A CTA takes T consecutive
 // tokens.  It first puts the cosines and sines of its tokens' pairs into shared memory - all heads share them, and evaluating
 // them per head would cost more instructions than everything else.  Then a thread keeps one place of the head (16 elements, both
-// halves of eight pairs in either pair layout) of one token, with the pairs' factors in registers, and walks over heads: q, k and
-// v alike, two 16-byte loads and two 16-byte stores per destination each, three heads' loads in flight.
+// halves of eight pairs in either pair layout) of one token, with the pairs' factors in registers, and walks over heads: two
+// 16-byte loads and two 16-byte stores per destination each, the next heads' loads in flight.  The query heads come first: the
+// chain of look-ups that ends in the token's cache row (sequence, block, slot: three dependent loads) hides behind them.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -24,7 +25,7 @@ namespace pie {
 namespace {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_AHEAD = 3;        // heads whose loads are in flight
+constexpr int ROPE_AHEAD = 2;        // query heads whose loads are in flight (and one of the keys' and values')
 
 struct RopeParams {
     RopeTable table;
@@ -84,7 +85,7 @@ __device__ __forceinline__ uint2 rope_pack8(const float (&x)[8], float scale, fl
 }
 
 template <int D, int T, bool BF16, bool KV8>
-__global__ void __launch_bounds__(ROPE_THREADS)
+__global__ void __launch_bounds__(ROPE_THREADS, 4)
 rope_kv_kernel(const __grid_constant__ RopeParams p) {
     constexpr int PLACES = D / 16, LANES = ROPE_THREADS / (PLACES * T);   // threads per head and token; heads side by side
     __shared__ __align__(16) float2 cs[T][D / 2];
@@ -93,20 +94,54 @@ rope_kv_kernel(const __grid_constant__ RopeParams p) {
     const int64_t t0 = (int64_t)blockIdx.x * T;
     const int nt = (int)min((int64_t)T, p.n_tokens - t0);
     const int pairs = p.table.rotary_dim >> 1;
+    const int j = tid % PLACES, tt = tid / PLACES % T, lane = tid / (PLACES * T);
+    const int64_t t = t0 + tt;
+    const bool live = tt < nt;
+    const int hq = live && p.q != nullptr ? p.n_q_heads : 0, hk = p.k != nullptr ? p.n_kv_heads : 0;
+    const int hkv = live ? hk + (p.block_table != nullptr ? p.n_kv_heads : 0) : 0;   // the key heads, then the value heads
+    const int rot = p.table.rotary_dim >> 4;
+    const bool turned = j < rot, adjacent = p.table.adjacent != 0;
+    // the two vectors of eight that a turned place consists of (one that is passed through: 2 j, 2 j + 1)
+    const int ta = turned && !adjacent ? j : 2 * j, tb = turned && !adjacent ? j + rot : 2 * j + 1;
+    const uint16_t *src_q = p.q + t * p.q_stride, *src_k = p.k + t * p.k_stride, *src_v = p.v + t * p.v_stride;
+    auto load_q = [&](int head, uint4 &wa, uint4 &wb) {
+        const uint4 *row = reinterpret_cast<const uint4 *>(src_q + head * D);
+        wa = row[ta];
+        wb = row[tb];
+    };
+    auto load_kv = [&](int head, uint4 &wa, uint4 &wb) {
+        const bool is_v = head >= hk;
+        const uint4 *row = reinterpret_cast<const uint4 *>(is_v ? src_v + (head - hk) * D : src_k + head * D);
+        wa = row[is_v ? 2 * j : ta];
+        wb = row[is_v ? 2 * j + 1 : tb];
+    };
+    uint4 qa[ROPE_AHEAD], qb[ROPE_AHEAD], ka, kb;
+#pragma unroll
+    for (int u = 0; u < ROPE_AHEAD; ++u)
+        if (lane + u * LANES < hq) load_q(lane + u * LANES, qa[u], qb[u]);   // (in flight while the factors are worked out)
+    if (lane < hkv) load_kv(lane, ka, kb);
 
-    for (int i = tid; i < T * (D / 2); i += ROPE_THREADS) {
-        const int tt = i / (D / 2), pr = i % (D / 2);
-        if (tt < nt && pr < pairs) {
-            const int32_t pos = __ldg(p.positions + p.table.axis[pr] * p.n_tokens + t0 + tt);
-            const unsigned long long turn = (unsigned long long)(long long)pos * p.table.turns[pr];
-            float s, c;
-            sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &s, &c);   // 2^-31: half turns
-            cs[tt][pr] = make_float2(c * p.table.amplitude, s * p.table.amplitude);
+    // the last warp's first lanes look the tokens' places up; the other warps work the factors out
+    const int look = p.block_table != nullptr && tid >= ROPE_THREADS - 32 ? tid & 31 : T;
+    int32_t s = 0, pos = 0;
+    if (look < nt) {
+        s = __ldg(p.token_seq + t0 + look);
+        pos = __ldg(p.token_pos + t0 + look);
+    }
+    if (tid < ROPE_THREADS - 32) {
+        for (int i = tid; i < T * (D / 2); i += ROPE_THREADS - 32) {
+            const int it = i / (D / 2), pr = i % (D / 2);
+            if (it < nt && pr < pairs) {
+                const int32_t at = __ldg(p.positions + p.table.axis[pr] * p.n_tokens + t0 + it);
+                const unsigned long long turn = (unsigned long long)(long long)at * p.table.turns[pr];
+                float sn, cn;
+                sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &sn, &cn);   // 2^-31: half turns
+                cs[it][pr] = make_float2(cn * p.table.amplitude, sn * p.table.amplitude);
+            }
         }
     }
-    if (p.block_table != nullptr && tid >= ROPE_THREADS - 32 && (tid & 31) < nt) {
-        const int tt = tid & 31;
-        const int32_t s = __ldg(p.token_seq + t0 + tt), pos = __ldg(p.token_pos + t0 + tt);
+    __syncthreads();   // the factors
+    if (look < nt) {   // (the places are wanted behind the query heads only)
         int32_t at = -1;
         if (s < 0 || s >= p.n_seqs || pos < 0 || (pos >> 4) >= p.max_blocks) {
             *reinterpret_cast<volatile int32_t *>(p.status + 1) = 1;
@@ -116,35 +151,9 @@ rope_kv_kernel(const __grid_constant__ RopeParams p) {
             if (slot < 0 || slot >= p.n_gpu_slots) *reinterpret_cast<volatile int32_t *>(p.status) = 1;
             else at = slot * 16 + (pos & 15);
         }
-        place[tt] = at;
+        place[look] = at;
     }
-
-    const int j = tid % PLACES, tt = tid / PLACES % T, lane = tid / (PLACES * T);
-    const int64_t t = t0 + tt;
-    const bool live = tt < nt;
-    const int hq = p.q != nullptr ? p.n_q_heads : 0, hk = p.k != nullptr ? p.n_kv_heads : 0;
-    const int hv = p.block_table != nullptr ? p.n_kv_heads : 0;
-    const int heads = live ? hq + hk + hv : 0;
-    const int rot = p.table.rotary_dim >> 4;
-    const bool turned = j < rot, adjacent = p.table.adjacent != 0;
-    // the two vectors of eight that a turned place consists of, and those of one that is passed through
-    const int ta = adjacent ? 2 * j : j, tb = adjacent ? 2 * j + 1 : j + rot;
-    auto load = [&](int head, uint4 &wa, uint4 &wb) {
-        const bool is_v = head >= hq + hk;
-        const uint16_t *src = head < hq ? p.q + t * p.q_stride + head * D : is_v ? p.v + t * p.v_stride + (head - hq - hk) * D : p.k + t * p.k_stride + (head - hq) * D;
-        const uint4 *row = reinterpret_cast<const uint4 *>(src);
-        const bool turn = turned && !is_v;
-        wa = row[turn ? ta : 2 * j];
-        wb = row[turn ? tb : 2 * j + 1];
-    };
-    uint4 wa[ROPE_AHEAD], wb[ROPE_AHEAD];
-#pragma unroll
-    for (int u = 0; u < ROPE_AHEAD; ++u)
-        if (lane + u * LANES < heads) load(lane + u * LANES, wa[u], wb[u]);   // (in flight while the factors are worked out)
-    __syncthreads();
     float2 c[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = make_float2(1.f, 0.f);
     if (turned && live) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -153,63 +162,77 @@ rope_kv_kernel(const __grid_constant__ RopeParams p) {
             c[2 * e + 1] = make_float2(f.z, f.w);
         }
     }
-    const int32_t at = hv != 0 && live ? place[tt] : -1;
-    for (int h0 = lane; h0 < heads; h0 += ROPE_AHEAD * LANES) {
+    auto turn = [&](uint4 &wa, uint4 &wb, float (&a)[8], float (&b)[8]) {
+        rope_unpack<BF16>(wa, a);
+        rope_unpack<BF16>(wb, b);
+        if (adjacent) {
 #pragma unroll
-        for (int u = 0; u < ROPE_AHEAD; ++u) {
-            const int head = h0 + u * LANES;
-            if (head >= heads) break;
-            const bool is_q = head < hq, is_v = head >= hq + hk, turn = turned && !is_v;
-            const int h = is_q ? head : is_v ? head - hq - hk : head - hq;
-            const int va = turn ? ta : 2 * j, vb = turn ? tb : 2 * j + 1;
-            float a[8], b[8];
-            if (turn || (KV8 && !is_q)) {
-                rope_unpack<BF16>(wa[u], a);
-                rope_unpack<BF16>(wb[u], b);
+            for (int e = 0; e < 4; ++e) {
+                const float x0 = a[2 * e], y0 = a[2 * e + 1], x1 = b[2 * e], y1 = b[2 * e + 1];
+                a[2 * e] = x0 * c[e].x - y0 * c[e].y;
+                a[2 * e + 1] = y0 * c[e].x + x0 * c[e].y;
+                b[2 * e] = x1 * c[4 + e].x - y1 * c[4 + e].y;
+                b[2 * e + 1] = y1 * c[4 + e].x + x1 * c[4 + e].y;
             }
-            if (turn) {
-                if (adjacent) {
+        } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float x0 = a[2 * e], y0 = a[2 * e + 1], x1 = b[2 * e], y1 = b[2 * e + 1];
-                        a[2 * e] = x0 * c[e].x - y0 * c[e].y;
-                        a[2 * e + 1] = y0 * c[e].x + x0 * c[e].y;
-                        b[2 * e] = x1 * c[4 + e].x - y1 * c[4 + e].y;
-                        b[2 * e + 1] = y1 * c[4 + e].x + x1 * c[4 + e].y;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = a[e], y = b[e];
-                        a[e] = x * c[e].x - y * c[e].y;
-                        b[e] = y * c[e].x + x * c[e].y;
-                    }
-                }
-                wa[u] = rope_pack<BF16>(a);
-                wb[u] = rope_pack<BF16>(b);
-            }
-            if (!is_v && (is_q || p.k_out != nullptr)) {
-                uint4 *dst = reinterpret_cast<uint4 *>(is_q ? p.q_out + (t * p.n_q_heads + h) * D : p.k_out + (t * p.n_kv_heads + h) * D);
-                dst[va] = wa[u];
-                dst[vb] = wb[u];
-            }
-            if (!is_q && at >= 0) {
-                const int64_t cache_row = (((int64_t)(at >> 4) * p.n_kv_heads + h) * 2 + (is_v ? 1 : 0)) * 16 + (at & 15);
-                if (KV8) {
-                    const float sc = is_v ? p.v_scale : p.k_scale, inv = is_v ? p.v_inv : p.k_inv;
-                    uint2 *dst = reinterpret_cast<uint2 *>(p.pool + cache_row * D);
-                    dst[va] = rope_pack8(a, sc, inv);
-                    dst[vb] = rope_pack8(b, sc, inv);
-                } else {
-                    uint4 *dst = reinterpret_cast<uint4 *>(p.pool + cache_row * D * 2);
-                    dst[va] = wa[u];
-                    dst[vb] = wb[u];
-                }
+            for (int e = 0; e < 8; ++e) {
+                const float x = a[e], y = b[e];
+                a[e] = x * c[e].x - y * c[e].y;
+                b[e] = y * c[e].x + x * c[e].y;
             }
         }
+        wa = rope_pack<BF16>(a);
+        wb = rope_pack<BF16>(b);
+    };
+    for (int h0 = lane; h0 < hq; h0 += ROPE_AHEAD * LANES) {
 #pragma unroll
-        for (int u = 0; u < ROPE_AHEAD; ++u)
-            if (h0 + (ROPE_AHEAD + u) * LANES < heads) load(h0 + (ROPE_AHEAD + u) * LANES, wa[u], wb[u]);
+        for (int u = 0; u < ROPE_AHEAD; ++u) {
+            const int h = h0 + u * LANES;
+            if (h < hq) {
+                if (turned) {
+                    float a[8], b[8];
+                    turn(qa[u], qb[u], a, b);
+                }
+                uint4 *dst = reinterpret_cast<uint4 *>(p.q_out + (t * p.n_q_heads + h) * D);
+                dst[ta] = qa[u];
+                dst[tb] = qb[u];
+                if (h + ROPE_AHEAD * LANES < hq) load_q(h + ROPE_AHEAD * LANES, qa[u], qb[u]);
+            }
+        }
+    }
+    __syncthreads();   // the tokens' places
+    const int32_t at = p.block_table != nullptr && live ? place[tt] : -1;
+    for (int head = lane; head < hkv; head += LANES) {
+        const bool is_v = head >= hk;
+        const int h = is_v ? head - hk : head, va = is_v ? 2 * j : ta, vb = is_v ? 2 * j + 1 : tb;
+        uint4 wa = ka, wb = kb;
+        if (head + LANES < hkv) load_kv(head + LANES, ka, kb);
+        float a[8], b[8];
+        if (turned && !is_v) {
+            turn(wa, wb, a, b);
+        } else if (KV8) {
+            rope_unpack<BF16>(wa, a);
+            rope_unpack<BF16>(wb, b);
+        }
+        if (!is_v && p.k_out != nullptr) {
+            uint4 *dst = reinterpret_cast<uint4 *>(p.k_out + (t * p.n_kv_heads + h) * D);
+            dst[va] = wa;
+            dst[vb] = wb;
+        }
+        if (at >= 0) {
+            const int64_t cache_row = (((int64_t)(at >> 4) * p.n_kv_heads + h) * 2 + (is_v ? 1 : 0)) * 16 + (at & 15);
+            if (KV8) {
+                const float sc = is_v ? p.v_scale : p.k_scale, inv = is_v ? p.v_inv : p.k_inv;
+                uint2 *dst = reinterpret_cast<uint2 *>(p.pool + cache_row * D);
+                dst[va] = rope_pack8(a, sc, inv);
+                dst[vb] = rope_pack8(b, sc, inv);
+            } else {
+                uint4 *dst = reinterpret_cast<uint4 *>(p.pool + cache_row * D * 2);
+                dst[va] = wa;
+                dst[vb] = wb;
+            }
+        }
     }
 }
 
@@ -277,7 +300,7 @@ cudaError_t launch_rope_kv(const AttnShape &sh, const RopeLaunch &a, const RopeT
     p.k_inv = exact_inverse(a.k_scale);
     p.v_inv = exact_inverse(a.v_scale);
     // Four tokens per CTA once that still gives every SM several CTAs; below, one: a decode step's latency is what counts there
-    return dispatch_rope(sh, a.n_tokens < 16 * n_sms, [&](auto kernel, int tokens) {
+    return dispatch_rope(sh, a.n_tokens < 4 * n_sms, [&](auto kernel, int tokens) {
         const int64_t grid = (a.n_tokens + tokens - 1) / tokens;
         if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
         kernel<<<(unsigned)grid, ROPE_THREADS, 0, stream>>>(p);
