@@ -420,10 +420,11 @@ int pie_prompt_plan(const int32_t *offsets, int32_t n_seqs, int32_t item_tokens,
  *     weights[s][kvh][t] += sum over the group's heads h of softmax_t(scale * q[s][h] . k[t])
  * weights: device fp32 [n_seqs][n_kv_heads][weights_stride]; entries at and behind ctx_len are left as they were (the caller
  * clears the entry of a new token, or starts from zeros).  The sums are formed in one fixed order: the same bits every time,
- * wherever the blocks lie.  out and the append are pie_decode_attention's (block_table_host .. v_new may be NULL).  A
+ * wherever the blocks lie.  out and the append are pie_decode_attention's (block_table_host .. v_new may be NULL); where the
+ * library chooses the split-K chunk it may take a shorter one here, and out may then differ in its last bits.  A
  * context longer than weights_stride: PIE_ERR_INVALID with host lengths; without them the entries beyond are dropped and the
  * next call returns PIE_ERR_INVALID.  PIE_ERR_UNSUPPORTED while the compute stream is being captured.  The first call on a
- * pool allocates its score scratch (4 * n_q_heads bytes per token of the pool). */
+ * pool allocates its scratch (about 4 * n_q_heads bytes per token of the pool, some 20 MiB at least). */
 int pie_decode_attention_weights(pie_pool *pool, int32_t layer, const void *q, void *out, const int32_t *block_table_dev,
                                  int32_t max_blocks_per_seq, const int32_t *ctx_lens_dev, const int32_t *block_table_host,
                                  const int32_t *ctx_lens_host, int32_t n_seqs, float scale, const void *k_new,

@@ -1351,27 +1351,19 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
 constexpr int COMB_THREADS = 64;
 constexpr int COMB_CAP = 256;  // chunks per sequence handled through shared memory; beyond that, plain loops
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(COMB_THREADS)
-combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, const int32_t *__restrict__ chunk_off,
-               uint16_t *__restrict__ out, int32_t n_q_heads, int32_t n_kv_heads, int32_t group, int32_t cap) {
-    extern __shared__ __align__(16) float comb_smem[];   // wbuf[group][cap], lbuf[group][cap]
+// One unit of the merge: slice `slice` of `slices` of head_dim of pair (s, kvh), by NT threads.
+template <int D, bool BF16, int NT>
+__device__ __forceinline__ void combine_unit(float *comb_smem, int tid, int32_t s, int32_t kvh, int slice, int slices, const float *__restrict__ part_o,
+                                             const float *__restrict__ part_ml, const int32_t *__restrict__ chunk_off, uint16_t *__restrict__ out,
+                                             int32_t n_q_heads, int32_t n_kv_heads, int32_t group, int32_t cap) {
     float *wbuf = comb_smem, *lbuf = comb_smem + group * cap;
-    // Launched with programmatic stream serialization: CTAs may become resident while the attention kernel still runs
-    // (which hides the launch); nothing that kernel wrote is read before the wait, which returns once the attention
-    // grid has completed and its writes are visible.  The kernel after this one may be launched the same way: let its
-    // CTAs become resident as soon as this grid's have started (it touches nothing of ours before its own wait).
-    grid_launch_dependents();
-    grid_dependency_wait();
-    const int tid = threadIdx.x;
-    const int32_t s = blockIdx.x / n_kv_heads, kvh = blockIdx.x - s * n_kv_heads;
     const int32_t chunk0 = chunk_off[s], nchunks = chunk_off[s + 1] - chunk0;
     if (nchunks < 2) return;
-    const int width = D / (int)gridDim.y;  // this CTA's slice of head_dim
-    const int d_lo = blockIdx.y * width;
+    const int width = D / slices;  // this CTA's slice of head_dim
+    const int d_lo = slice * width;
     const int64_t row0 = ((int64_t)s * n_q_heads + (int64_t)kvh * group) * D;
     if (nchunks <= cap) {
-        for (int idx = tid; idx < group * nchunks; idx += COMB_THREADS) {
+        for (int idx = tid; idx < group * nchunks; idx += NT) {
             const int g = idx / nchunks, c = idx - g * nchunks;
             const int64_t id = ((int64_t)(chunk0 + c) * n_kv_heads + kvh) * group + g;
             wbuf[g * cap + c] = part_ml[id * 2];
@@ -1381,7 +1373,7 @@ combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_
         // every thread works the weights of its head out for itself (a few exponentials, in chunk order: the same
         // sums whichever thread forms them), so there is no serial pass over the chunks between two barriers
         const int per_head = width / 4;   // float4 pieces per head in the slice
-        for (int e4 = tid; e4 < group * per_head; e4 += COMB_THREADS) {
+        for (int e4 = tid; e4 < group * per_head; e4 += NT) {
             const int g = e4 / per_head, d = d_lo + (e4 - g * per_head) * 4;
             const float *w = wbuf + g * cap, *l = lbuf + g * cap;
             const uint2 r = merge_piece<D, BF16>(part_o, chunk0, nchunks, n_kv_heads, kvh, group, g, d,
@@ -1390,7 +1382,7 @@ combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_
         }
         return;
     }
-    for (int e = tid; e < group * width; e += COMB_THREADS) {  // very many chunks: plain loops
+    for (int e = tid; e < group * width; e += NT) {  // very many chunks: plain loops
         const int g = e / width, d = d_lo + (e - g * width);
         float mm = -INFINITY;
         for (int32_t c = 0; c < nchunks; ++c) mm = fmaxf(mm, part_ml[(((int64_t)(chunk0 + c) * n_kv_heads + kvh) * group + g) * 2]);
@@ -1407,58 +1399,128 @@ combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_
     }
 }
 
-// =====================================================================================================
-// Attention weights: the attention kernel has left every score (log2 units) and every chunk's maximum and sum per head;
-// a token's weight is the sum over its group's heads of 2^(score - m) / l, with m and l merged over the sequence's chunks.
-// Storing the scores costs 8 bytes per (token, query head), written and read once and mostly from L2; computing them again
-// from the keys would cost half of the cache's bytes a second time.  One CTA per item (chunk, KV head), items in turn.
-// =====================================================================================================
-constexpr int WEIGHTS_THREADS = 128;
-
-__global__ void __launch_bounds__(WEIGHTS_THREADS)
-attn_weights_kernel(const float *__restrict__ scores, const float *__restrict__ part_ml, const int32_t *__restrict__ chunk_off,
-                    const int32_t *__restrict__ ctx_lens, float *__restrict__ weights, int64_t stride, int32_t n_seqs, int32_t n_kv_heads,
-                    int32_t group, int32_t split_tokens, int32_t max_tokens, int32_t *status) {
-    __shared__ float sh_m[8], sh_inv[8];
+template <int D, bool BF16>
+__global__ void __launch_bounds__(COMB_THREADS)
+combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, const int32_t *__restrict__ chunk_off,
+               uint16_t *__restrict__ out, int32_t n_q_heads, int32_t n_kv_heads, int32_t group, int32_t cap) {
+    extern __shared__ __align__(16) float comb_smem[];   // wbuf[group][cap], lbuf[group][cap]
+    // Launched with programmatic stream serialization: CTAs may become resident while the attention kernel still runs
+    // (which hides the launch); nothing that kernel wrote is read before the wait, which returns once the attention
+    // grid has completed and its writes are visible.  The kernel after this one may be launched the same way: let its
+    // CTAs become resident as soon as this grid's have started (it touches nothing of ours before its own wait).
     grid_launch_dependents();
     grid_dependency_wait();
-    const int tid = threadIdx.x;
+    const int32_t s = blockIdx.x / n_kv_heads, kvh = blockIdx.x - s * n_kv_heads;
+    combine_unit<D, BF16, COMB_THREADS>(comb_smem, threadIdx.x, s, kvh, blockIdx.y, gridDim.y, part_o, part_ml, chunk_off, out, n_q_heads, n_kv_heads,
+                                        group, cap);
+}
+
+// =====================================================================================================
+// What follows the attention kernel of a call that accumulates attention weights: the merge of the chunks' outputs (as the
+// combine kernel does it) and the weights, side by side in one launch.
+//
+// The attention kernel has left every score (log2 units) and every chunk's maximum and sum per head; a token's weight is the sum
+// over its group's heads of 2^(score - m) / l, with m and l merged over the sequence's chunks.  Storing the scores costs 8 bytes
+// per (token, query head), written and read once and mostly from L2; computing them again from the keys would cost half of the
+// cache's bytes a second time.  A piece of an item (chunk, KV head) per warp, as many tokens as a lane's 16 scores cover, without a
+// barrier and in few dependent steps: the scores go into registers while the sequence is looked up (every lane compares some of the
+// chunk offsets), then the weights so far and all heads' maxima and sums (a lane per chunk) are fetched at once.
+// =====================================================================================================
+constexpr int FIN_THREADS = 128;
+constexpr int FIN_HELD = 16;   // scores that a lane holds
+
+template <int D, bool BF16, int G>
+__global__ void __launch_bounds__(FIN_THREADS)
+attn_finish_kernel(const float *__restrict__ scores, const float *__restrict__ part_o, const float *__restrict__ part_ml,
+                   const int32_t *__restrict__ chunk_off, const int32_t *__restrict__ ctx_lens, uint16_t *__restrict__ out,
+                   float *__restrict__ weights, int64_t stride, int32_t n_seqs, int32_t n_kv_heads, int32_t split_tokens, int32_t max_tokens,
+                   int32_t cap, int32_t slices, int32_t merge_ctas, int32_t *status) {
+    extern __shared__ __align__(16) float comb_smem[];
+    constexpr int AHEAD = G >= FIN_HELD ? 1 : FIN_HELD / G;   // tokens of a lane at a time
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if ((int32_t)blockIdx.x < merge_ctas) {   // the merge first: its chain of loads is the longer one
+        const int32_t unit = (int32_t)blockIdx.x, pair = unit / slices, s = pair / n_kv_heads;
+        combine_unit<D, BF16, FIN_THREADS>(comb_smem, tid, s, pair - s * n_kv_heads, unit - pair * slices, slices, part_o, part_ml, chunk_off, out,
+                                           n_kv_heads * G, n_kv_heads, G, cap);
+        return;
+    }
     const int32_t n_items = chunk_off[n_seqs] * n_kv_heads;
-    for (int32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const int32_t pieces = (split_tokens + AHEAD * 32 - 1) / (AHEAD * 32);
+    const int32_t weight_ctas = (int32_t)gridDim.x - merge_ctas;
+    for (int64_t piece = (int64_t)((int32_t)blockIdx.x - merge_ctas) * (FIN_THREADS / 32) + warp; piece < (int64_t)n_items * pieces; piece += (int64_t)weight_ctas * (FIN_THREADS / 32)) {
+        const int32_t item = (int32_t)(piece / pieces), base = (int32_t)(piece - (int64_t)item * pieces) * AHEAD * 32;
         const int32_t ci = item / n_kv_heads, kvh = item - ci * n_kv_heads;
-        int32_t lo = 0, hi = n_seqs;  // largest s with chunk_off[s] <= ci
-        while (hi - lo > 1) {
-            const int32_t mid = (lo + hi) >> 1;
-            if (chunk_off[mid] <= ci) lo = mid;
-            else hi = mid;
+        // the scores: their place depends on nothing but the item (beyond the chunk's end: not used)
+        const float *sc = scores + (int64_t)item * split_tokens * G;
+        float v[AHEAD][G];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int32_t t = base + u * 32 + lane;
+            if (t < split_tokens) {
+                if constexpr (G % 4 == 0) {
+#pragma unroll
+                    for (int g = 0; g < G; g += 4) {
+                        const float4 x = *reinterpret_cast<const float4 *>(sc + (int64_t)t * G + g);
+                        v[u][g] = x.x, v[u][g + 1] = x.y, v[u][g + 2] = x.z, v[u][g + 3] = x.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int g = 0; g < G; ++g) v[u][g] = sc[(int64_t)t * G + g];
+                }
+            }
         }
-        const int32_t chunk0 = chunk_off[lo], nchunks = chunk_off[lo + 1] - chunk0;
-        const int32_t ctx = min(__ldg(ctx_lens + lo), max_tokens);
+        // the item's sequence: the largest s with chunk_off[s] <= ci
+        int32_t seen = 0;
+        for (int32_t b = 0; b < n_seqs; b += 32)
+            seen += __popc(__ballot_sync(0xffffffffu, b + lane < n_seqs && __ldg(chunk_off + b + lane) <= ci));
+        const int32_t s = seen - 1;
+        const int32_t chunk0 = chunk_off[s], nchunks = chunk_off[s + 1] - chunk0;
+        const int32_t ctx = min(__ldg(ctx_lens + s), max_tokens);
         const int64_t t0 = (int64_t)(ci - chunk0) * split_tokens;
         int32_t n = (int32_t)min((int64_t)split_tokens, ctx - t0);
         if (t0 + n > stride) {   // no room for these tokens' weights
-            if (tid == 0) raise_status(status, STATUS_CTX_TOO_LONG);
+            if (lane == 0) raise_status(status, STATUS_CTX_TOO_LONG);
             n = (int32_t)max((int64_t)0, stride - t0);
         }
-        if (tid < group) {   // merged over the chunks in chunk order
-            float mm = -INFINITY, ll = 0.f;
-            for (int32_t c = 0; c < nchunks; ++c) mm = fmaxf(mm, part_ml[((((int64_t)chunk0 + c) * n_kv_heads + kvh) * group + tid) * 2]);
-            for (int32_t c = 0; c < nchunks; ++c) {
-                const int64_t id = ((((int64_t)chunk0 + c) * n_kv_heads + kvh) * group + tid) * 2;
-                ll += part_ml[id + 1] * (part_ml[id] == -INFINITY ? 0.f : fast_exp2(part_ml[id] - mm));
+        float *wrow = weights + ((int64_t)s * n_kv_heads + kvh) * stride + t0;
+        const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + ((int64_t)chunk0 * n_kv_heads + kvh) * G;
+        const int64_t ml_chunk = (int64_t)n_kv_heads * G;
+        float old[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) old[u] = base + u * 32 + lane < n ? wrow[base + u * 32 + lane] : 0.f;
+        float2 x[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) x[g] = lane < nchunks ? ml[lane * ml_chunk + g] : make_float2(-INFINITY, 0.f);
+        float m_all[G], inv[G];
+        auto join = [](float &mm, float &ll, float m2, float l2) {   // (the same sum from either side)
+            const float m = fmaxf(mm, m2);
+            ll = m == -INFINITY ? ll + l2 : ll * fast_exp2(mm - m) + l2 * fast_exp2(m2 - m);
+            mm = m;
+        };
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float mm = x[g].x, ll = x[g].y;
+            for (int32_t c = lane + 32; c < nchunks; c += 32) {
+                const float2 y = ml[c * ml_chunk + g];
+                join(mm, ll, y.x, y.y);
             }
-            sh_m[tid] = mm;
-            sh_inv[tid] = 1.f / ll;
+            for (int o = 1; o < 32 && o < nchunks; o <<= 1)   // (lanes beyond the chunks hold nothing)
+                join(mm, ll, __shfl_xor_sync(0xffffffffu, mm, o), __shfl_xor_sync(0xffffffffu, ll, o));
+            m_all[g] = __shfl_sync(0xffffffffu, mm, 0);
+            inv[g] = 1.f / __shfl_sync(0xffffffffu, ll, 0);
         }
-        __syncthreads();
-        float *wrow = weights + ((int64_t)lo * n_kv_heads + kvh) * stride + t0;
-        const float *sc = scores + (int64_t)item * split_tokens * group;
-        for (int32_t t = tid; t < n; t += WEIGHTS_THREADS) {
-            float w = 0.f;
-            for (int g = 0; g < group; ++g) w += fast_exp2(sc[(int64_t)t * group + g] - sh_m[g]) * sh_inv[g];
-            wrow[t] += w;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int32_t t = base + u * 32 + lane;
+            if (t < n) {
+                float w = 0.f;
+#pragma unroll
+                for (int g = 0; g < G; ++g) w += fast_exp2(v[u][g] - m_all[g]) * inv[g];
+                wrow[t] = old[u] + w;
+            }
         }
-        __syncthreads();
     }
 }
 
@@ -1607,9 +1669,33 @@ static cudaError_t dispatch_weights(int head_dim, int dtype, int kv_fp8, F &&f) 
                              : f(paged_decode_attn_kernel<64, false, 4, 2, false, true>, AttnSmem<64, 4, 2>::BYTES, 2);
 }
 
+template <typename F>
+static cudaError_t dispatch_finish(int head_dim, int dtype, int group, F &&f) {
+#define PIE_FINISH(GV)                                                                                                          \
+    case GV:                                                                                                                    \
+        if (head_dim == 128) return dtype == PIE_BF16 ? f(attn_finish_kernel<128, true, GV>) : f(attn_finish_kernel<128, false, GV>); \
+        return dtype == PIE_BF16 ? f(attn_finish_kernel<64, true, GV>) : f(attn_finish_kernel<64, false, GV>);
+    switch (group) {
+        PIE_FINISH(1)
+        PIE_FINISH(2)
+        PIE_FINISH(3)
+        PIE_FINISH(4)
+        PIE_FINISH(5)
+        PIE_FINISH(6)
+        PIE_FINISH(7)
+        PIE_FINISH(8)
+        default: return cudaErrorInvalidValue;
+    }
+#undef PIE_FINISH
+}
+
 cudaError_t attn_weights_configure(int head_dim, int dtype, int *ctas_per_sm, int kv_fp8) {
-    cudaError_t e0 = cudaFuncSetAttribute(attn_weights_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    if (e0 != cudaSuccess) return e0;
+    for (int g = 1; g <= 8; ++g) {
+        const cudaError_t e0 = dispatch_finish(head_dim, dtype, g, [](auto kernel) {
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        });
+        if (e0 != cudaSuccess) return e0;
+    }
     return dispatch_weights(head_dim, dtype, kv_fp8, [&](auto kernel, int smem, int nw) -> cudaError_t {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
@@ -1685,20 +1771,31 @@ cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const A
             kernel<<<a.grid, (nw + 1) * 32, smem, stream>>>(map, p);
             return cudaGetLastError();
         });
-        if (ew == cudaSuccess) ew = launch_combine(sh, sc, a.out, a.n_seqs, a.max_blocks, a.split_tokens, turn, stream);
         if (ew != cudaSuccess) return ew;
+        const int32_t group = p.group;
+        const int64_t longest = ((int64_t)a.max_blocks * 16 + a.split_tokens - 1) / a.split_tokens;   // chunks, as in launch_combine
+        const int32_t cap = (int32_t)std::min<int64_t>(COMB_CAP, (longest + 7) / 8 * 8);
+        int32_t slices = 1;
+        while (slices < sh.head_dim / 32 && group * (sh.head_dim / 4) / slices > FIN_THREADS) slices *= 2;
+        const int32_t merge_ctas = longest > 1 ? a.n_seqs * sh.n_kv_heads * slices : 0;
+        const int32_t ahead = FIN_HELD / group > 0 ? FIN_HELD / group : 1, pieces = (a.split_tokens + ahead * 32 - 1) / (ahead * 32);
+        const int32_t weight_ctas =
+            (int32_t)std::min<int64_t>(((int64_t)a.n_seqs * longest * sh.n_kv_heads * pieces + FIN_THREADS / 32 - 1) / (FIN_THREADS / 32), 1 << 20);
         cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3((unsigned)std::min<int64_t>(sc.max_items, 8 * (int64_t)a.grid));
-        lc.blockDim = dim3(WEIGHTS_THREADS);
+        lc.gridDim = dim3((unsigned)(weight_ctas + merge_ctas));
+        lc.blockDim = dim3(FIN_THREADS);
+        lc.dynamicSmemBytes = (size_t)(2 * group * cap) * sizeof(float);
         lc.stream = stream;
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at[0].val.programmaticStreamSerializationAllowed = 1;
         lc.attrs = at;
         lc.numAttrs = 1;
-        return cudaLaunchKernelEx(&lc, attn_weights_kernel, (const float *)sc.scores, (const float *)p.part_ml, (const int32_t *)sc.chunk_off,
-                                  a.ctx_lens, a.weights, a.weights_stride, a.n_seqs, sh.n_kv_heads, (int32_t)p.group, a.split_tokens,
-                                  a.max_blocks * 16, a.status);
+        return dispatch_finish(sh.head_dim, sh.dtype, group, [&](auto kernel) {
+            return cudaLaunchKernelEx(&lc, kernel, (const float *)sc.scores, (const float *)p.part_o, (const float *)p.part_ml,
+                                      (const int32_t *)sc.chunk_off, a.ctx_lens, (uint16_t *)a.out, a.weights, a.weights_stride, a.n_seqs,
+                                      sh.n_kv_heads, a.split_tokens, a.max_blocks * 16, cap, slices, merge_ctas, a.status);
+        });
     }
     cudaError_t e = dispatch_variant(sh.head_dim, sh.dtype, a.variant, sh.kv_fp8, [&](auto kernel, int smem, int nw) -> cudaError_t {
         if (!a.dependent_launch) {

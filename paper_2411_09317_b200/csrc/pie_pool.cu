@@ -138,6 +138,8 @@ struct pie_pool {
     pie::RopeTable rope{};       // rotary_dim 0: not set (pie_set_rope)
     int32_t *prompt_items = nullptr;   // host: the items of a small call
     int attn_weights_grid = 0;   // 0: not configured yet
+    pie::AttnScratch weights_scratch{};   // the scratch of calls that accumulate weights: room for eight items per CTA at least
+    int64_t weights_scores = 0;           // floats of its score buffer
     int32_t *evict_scratch = nullptr;   // per kept token its row, per (sequence, KV head) the number of them
     int64_t evict_words = 0;
     int device = 0;
@@ -806,7 +808,9 @@ void destroy_pool(pie_pool *p) {
     cudaFree(p->scratch.counters);
     cudaFree(p->scratch.part_o);
     cudaFree(p->scratch.part_ml);
-    cudaFree(p->scratch.scores);
+    cudaFree(p->weights_scratch.scores);
+    if (p->weights_scratch.part_o != p->scratch.part_o) cudaFree(p->weights_scratch.part_o);
+    if (p->weights_scratch.part_ml != p->scratch.part_ml) cudaFree(p->weights_scratch.part_ml);
     cudaFree(p->evict_scratch);
     delete[] p->prompt_items;
     for (int t = 0; t < 2; ++t) {
@@ -874,6 +878,18 @@ int attention_call(pie_pool *p, int32_t layer, const void *q, void *out, const i
                 break;
             }
     }
+    // Calls that accumulate weights: shorter chunks where the batch gives the CTAs few items (counted from what the table could
+    // hold: the lengths are on the device).  Below four items per CTA, halves down to 256 tokens even the CTAs out (64 sequences of
+    // up to 2000 tokens, 8-bit blocks: 55 -> 53 us; 32 of up to 4000, 16-bit, at 14 items per CTA, the other way round: 199 ->
+    // 211 us); below one, down to 32 tokens (one sequence of 333: 18.5 -> 12.4 us).
+    pie::AttnScratch scratch = weights ? p->weights_scratch : p->scratch;
+    if (weights && p->auto_split) {
+        auto items = [&](int64_t tokens) { return (int64_t)n_seqs * (((int64_t)max_blocks * 16 + tokens - 1) / tokens) * p->cfg.n_kv_heads; };
+        while ((split > 256 && items(split) < 4 * (int64_t)p->attn_weights_grid && items(split / 2) <= scratch.max_items) ||
+               (split > 32 && items(split) < p->attn_weights_grid))
+            split /= 2;
+    }
+    if (weights) scratch.max_items = std::min(scratch.max_items, p->weights_scores / (split * (p->cfg.n_q_heads / p->cfg.n_kv_heads)));
     // host-side checks when the caller supplied host copies of the tables
     int64_t ticket = 0, waits[4];
     if (bt_host) {
@@ -886,7 +902,7 @@ int attention_call(pie_pool *p, int32_t layer, const void *q, void *out, const i
             chunks += (ctx + split - 1) / split;
             for (int32_t b = 0; b < (ctx + 15) / 16; ++b) p->v_in.push_back(bt_host[(int64_t)s * max_blocks + b]);
         }
-        if (chunks * p->cfg.n_kv_heads > p->scratch.max_items) return PIE_ERR_INVALID;
+        if (chunks * p->cfg.n_kv_heads > scratch.max_items) return PIE_ERR_INVALID;
         st = p->table->attention(layer, p->v_in.data(), (int64_t)p->v_in.size(), &ticket, waits);
     } else {
         st = p->table->attention(layer, nullptr, 0, &ticket, waits);
@@ -974,7 +990,7 @@ int attention_call(pie_pool *p, int32_t layer, const void *q, void *out, const i
         const int k = (int)(p->step % TIMING_RING);
         if (cudaEventRecord(p->lev_anchor[k], stream) == cudaSuccess) p->lev_anchored[k] = true;
     }
-    cudaError_t e = pie::launch_attention(sh, p->scratch, a, p->use3d ? p->map3d : p->map2d, p->use3d, stream);
+    cudaError_t e = pie::launch_attention(sh, scratch, a, p->use3d ? p->map3d : p->map2d, p->use3d, stream);
     if (e != cudaSuccess) {
         g_last_cuda_error = (int)e;
         p->sticky = PIE_ERR_CUDA;
@@ -2251,15 +2267,31 @@ int pie_decode_attention_weights(pie_pool *pool, int32_t layer, const void *q, v
         PIE_CUDA(pie::attn_weights_configure(pool->cfg.head_dim, pool->cfg.dtype, &per_sm, pool->kv_fp8));
         if (per_sm <= 0) return PIE_ERR_UNSUPPORTED;
         if (pool->cfg.attn_ctas_per_sm > 0) per_sm = std::min(per_sm, pool->cfg.attn_ctas_per_sm);
-        const size_t bytes = (size_t)pool->scratch.max_items * (size_t)pool->cfg.split_tokens * (size_t)(pool->cfg.n_q_heads / pool->cfg.n_kv_heads) * 4;
-        const cudaError_t e = cudaMalloc((void **)&pool->scratch.scores, bytes);
+        const int grid = per_sm * pool->n_sms;
+        const size_t G = (size_t)(pool->cfg.n_q_heads / pool->cfg.n_kv_heads);
+        pie::AttnScratch w = pool->scratch;
+        cudaError_t e = cudaSuccess;
+        const int64_t scores = std::max<int64_t>(w.max_items * pool->cfg.split_tokens, 8 * (int64_t)grid * 256) * (int64_t)G;
+        if (w.max_items < 8 * (int64_t)grid) {   // a small pool: its partials would not hold a small batch's short chunks
+            w.max_items = 8 * (int64_t)grid;
+            w.part_o = w.part_ml = nullptr;
+            e = cudaMalloc((void **)&w.part_o, (size_t)w.max_items * G * (size_t)pool->cfg.head_dim * 4);
+            if (e == cudaSuccess) e = cudaMalloc((void **)&w.part_ml, (size_t)w.max_items * G * 2 * 4);
+        }
+        for (int t = 0; t < 2; ++t) w.part_o_more[t] = w.part_ml_more[t] = nullptr;   // (nothing is deferred)
+        if (e == cudaSuccess) e = cudaMalloc((void **)&w.scores, (size_t)scores * 4);
         if (e != cudaSuccess) {
             cudaGetLastError();   // (an allocation that failed leaves the device as it was)
-            pool->scratch.scores = nullptr;
+            if (w.part_o != pool->scratch.part_o) {
+                cudaFree(w.part_o);
+                cudaFree(w.part_ml);
+            }
             g_last_cuda_error = (int)e;
             return PIE_ERR_NOMEM;
         }
-        pool->attn_weights_grid = per_sm * pool->n_sms;
+        pool->weights_scratch = w;
+        pool->weights_scores = scores;
+        pool->attn_weights_grid = grid;
     }
     return attention_call(pool, layer, q, out, block_table_dev, max_blocks_per_seq, ctx_lens_dev, block_table_host, ctx_lens_host,
                           n_seqs, scale, k_new, v_new, false, false, false, weights, weights_stride);
