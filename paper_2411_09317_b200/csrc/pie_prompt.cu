@@ -76,32 +76,11 @@ __device__ __forceinline__ void pr_tma_3d(uint32_t dst, const CUtensorMap *map, 
         : "memory");
 }
 
-// tcgen05.mma / commit by the lane whose `leader` is not 0, without a branch
-__device__ __forceinline__ void pr_mma_ss(uint32_t leader, uint32_t tmem_d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, e;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "setp.ne.b32 e, %5, 0;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader)
-        : "memory");
-}
-__device__ __forceinline__ void pr_mma_ts(uint32_t leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, e;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "setp.ne.b32 e, %5, 0;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader)
-        : "memory");
-}
-__device__ __forceinline__ void pr_commit(uint32_t leader, uint32_t bar) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\t"
-        "setp.ne.b32 e, %1, 0;\n\t"
-        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
-        ::"r"(bar), "r"(leader)
-        : "memory");
+// true in one lane of the (whole) warp: the branch of an elected lane keeps the operands in uniform registers
+__device__ __forceinline__ bool pr_elect() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 
 // the larger of three; NaN if any of them is one
@@ -165,10 +144,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     using SM = PrSmem<D>;
     constexpr int HALVES = D / 64;
     constexpr int RING = SM::RING;
-    // Share of the exponentials, in eighths, that the arithmetic pipes take over from the special-function unit (16 a clock and SM,
-    // as many as the tensor core asks for with heads of 128).  More of them costs more instructions and more power than the unit's
-    // relief gives back: 10007 tokens, 32 heads: 0, 1, 2 eighths 702, 702, 731 us with heads of 128, 643, 634, 613 us with 64.
-    constexpr int POLY = D == 128 ? 1 : 2;
+    // Share of the exponentials, in eighths, that the arithmetic pipes take over from the special-function unit (16 a clock and SM:
+    // as long for a stage's exponentials as the tensor core for its products).  More of them costs more instructions and more
+    // power than the unit's relief gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128, after half a second of load: 0, 1,
+    // 2 eighths 802, 779, 774 us; 16 ragged prompts: 176, 162, 161 us; 3 eighths: 711 against 661 us before the clock falls.
+    constexpr int POLY = 2;
     extern __shared__ __align__(1024) uint8_t pr_smem[];
     uint8_t *smem = pr_smem;
     const uint32_t base = pf_smem_u32(pr_smem);
@@ -217,7 +197,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         for (int t = 0; t < 2; ++t) {
             pf_mbar_init(bar_q + 8 * t, 1);
             pf_mbar_init(bar_s + 8 * t, 1);
-            pf_mbar_init(bar_p + 8 * t, 128);
+            pf_mbar_init(bar_p + 8 * t, 4);   // a warp each
             pf_mbar_init(bar_done + 8 * t, 1);
         }
         misc[1] = 0;
@@ -331,22 +311,25 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         __syncwarp();
     } else if (warp == 8) {
         // =============================================================================== the issuing warp
-        // The descriptors are warp-uniform values, formed outside of any divergent branch (the instruction takes them from uniform
-        // registers: formed in the branch of one lane, each MMA waited some 30 cycles for the moves), and the lane that issues is a
-        // predicate of the instruction.  TMEM: all 512 columns are this CTA's, so its base is column 0.
+        // The operands are warp-uniform values and the branch is an elected lane's, so that the MMAs take them from uniform
+        // registers as they come: formed in the branch of lane 0, each MMA waited for the moves (863 us for 10007 tokens), issued
+        // without a branch, by a predicate, it cost some ten instructions (715 us; so 679 us).  TMEM: all 512 columns are this
+        // CTA's, so its base is column 0.
         constexpr uint32_t IDESC_S = instr_desc(BF16, PR_KV, false), IDESC_O = instr_desc(BF16, D, true);
-        const uint32_t leader = lane == 0 ? 1u : 0u;
         const uint64_t q_desc = smem_desc(base + SM::OFF_Q, 16, 1024), k_desc = smem_desc(base + SM::OFF_RING, 16, 1024);
         const uint64_t v_desc = smem_desc(base + SM::OFF_RING, PR_KV * 128, 1024);
         // S of a tile, K in ring slot `slot`
         auto issue_s = [&](int t, uint32_t slot) {
             tc_fence_after();
             const uint64_t qd = q_desc + (uint64_t)(t * (TC_M * D * 2) >> 4), kd = k_desc + (uint64_t)(slot * (SM::STAGE >> 4));
+            if (pr_elect()) {
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks)
-                pr_mma_ss(leader, t * 128, qd + (uint64_t)(((ks >> 2) * (TC_M * 128) + (ks & 3) * 32) >> 4),
-                          kd + (uint64_t)(((ks >> 2) * (PR_KV * 128) + (ks & 3) * 32) >> 4), IDESC_S, ks > 0 ? 1u : 0u);
-            pr_commit(leader, bar_s + 8 * t);
+                for (int ks = 0; ks < D / 16; ++ks)
+                    mma_f16(t * 128, qd + (uint64_t)(((ks >> 2) * (TC_M * 128) + (ks & 3) * 32) >> 4),
+                            kd + (uint64_t)(((ks >> 2) * (PR_KV * 128) + (ks & 3) * 32) >> 4), IDESC_S, ks > 0 ? 1u : 0u);
+                tc_commit(bar_s + 8 * t);
+            }
+            __syncwarp();
         };
         Item it, next;
         bool more = get_item(0, it), ok = true;
@@ -360,7 +343,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     q_count[t] = 1;
                     if (ok) issue_s(t, 0);
                 }
-            pr_commit(leader, bar_free);
+            if (pr_elect()) tc_commit(bar_free);
+            __syncwarp();
         }
         uint32_t v_slot = 1;
         int32_t g = 0;
@@ -380,10 +364,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         ++p_count[t];
                         if (!ok) continue;
                         tc_fence_after();
+                        if (pr_elect()) {
 #pragma unroll
-                        for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
-                            pr_mma_ts(leader, 256 + t * 128, t * 128 + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), IDESC_O, (j > 0 || ks > 0) ? 1u : 0u);
-                        if (j + 1 == n) pr_commit(leader, bar_done + 8 * t);
+                            for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
+                                mma_f16_ts(256 + t * 128, t * 128 + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), IDESC_O, (j > 0 || ks > 0) ? 1u : 0u);
+                            if (j + 1 == n) tc_commit(bar_done + 8 * t);
+                        }
+                        __syncwarp();
                     }
                     if (ok && (j + 1 < n || (last && nx > 0))) {   // the item's next scores, or the next item's first
                         if (j + 1 >= n) {
@@ -393,7 +380,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         if (ok) issue_s(t, k_slot);
                     }
                 }
-                pr_commit(leader, bar_free + 8 * ((g + 1) & 3));
+                if (pr_elect()) tc_commit(bar_free + 8 * ((g + 1) & 3));
+                __syncwarp();
                 v_slot = k_slot + 1 == RING ? 0 : k_slot + 1;
             }
             it = next;
@@ -472,6 +460,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     else s0 = pr_add2(s0, e);
                     pw[w] = pf_pack2<BF16>(e.x, e.y);
                 }
+                if (masked) {   // (the polynomial's smallest value is 2^-125: what is masked is nothing at all)
+#pragma unroll
+                    for (int w = 0; w < 32; ++w) {
+                        const int32_t more = my_pos - (t_base + 64 * h + 2 * w);
+                        pw[w] = more < 0 ? 0u : more == 0 ? pw[w] & 0xffffu : pw[w];
+                    }
+                }
                 tmem_st32(tmem_s + 32 * h, pw);   // a thread overwrites only its own row's scores, which it has read
             }
             s0 = pr_add2(s0, s1);
@@ -515,7 +510,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             tmem_wait_st();
             tc_fence_before();
-            pf_mbar_arrive(bar_p + 8 * t);
+            __syncwarp();
+            if (lane == 0) pf_mbar_arrive(bar_p + 8 * t);
         }
         if (ok) ok = wait_all(bar_done + 8 * t, done_count & 1u);
         ++done_count;

@@ -351,11 +351,12 @@ def test_prompt_scales(dtype, scale, k_gain):
 
 
 @pytest.mark.parametrize("dtype,d", [(F16, 128), (BF16, 128), (BF16, 64)])
-@pytest.mark.parametrize("value", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("value", ["nan", "inf", "-inf", "largest"])
 def test_prompt_masked_places_cannot_reach_a_row(dtype, d, value):
     """NaN and infinities in the keys and values of later tokens, and of other sequences, change nothing; rows that see such a
     value get what the definition gives (NaN or the infinity in the value's own column)."""
-    bits = {"nan": 0x7e00 if dtype == F16 else 0x7fc0, "inf": 0x7c00 if dtype == F16 else 0x7f80, "-inf": 0xfc00 if dtype == F16 else 0xff80}[value]
+    bits = {"nan": 0x7e00 if dtype == F16 else 0x7fc0, "inf": 0x7c00 if dtype == F16 else 0x7f80, "-inf": 0xfc00 if dtype == F16 else 0xff80,
+            "largest": 0x7bff if dtype == F16 else 0x7f7f}[value]
     lens, at = [200, 300, 64], {0: 150, 1: 17, 2: 63}
 
     def poison_v(k, v, off):
@@ -369,7 +370,10 @@ def test_prompt_masked_places_cannot_reach_a_row(dtype, d, value):
         assert np.array_equal(got[o:o + t], clean[o:o + t])
         assert np.array_equal(np.delete(got[o + t:e], 5, axis=2), np.delete(clean[o + t:e], 5, axis=2))
         seen = got[o + t:e, :, 5]
-        assert np.all(np.isnan(seen)) if value == "nan" else np.all(seen == (np.inf if value == "inf" else -np.inf))
+        if value == "nan":
+            assert np.all(np.isnan(seen))
+        elif value != "largest":
+            assert np.all(seen == (np.inf if value == "inf" else -np.inf))
 
     def poison_k(k, v, off):
         for s, t in at.items():
