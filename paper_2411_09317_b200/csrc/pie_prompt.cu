@@ -96,6 +96,13 @@ __device__ __forceinline__ float2 pr_fma2(float2 a, float2 b, float2 c) {
         : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
     return r;
 }
+__device__ __forceinline__ float2 pr_mul2(float2 a, float2 b) {
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(*reinterpret_cast<uint64_t *>(&r))
+        : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return r;
+}
 __device__ __forceinline__ float2 pr_add2(float2 a, float2 b) {
     float2 r;
     asm("add.rn.f32x2 %0, %1, %2;"
@@ -104,12 +111,13 @@ __device__ __forceinline__ float2 pr_add2(float2 a, float2 b) {
     return r;
 }
 
-// 2^x for two values at once, in the arithmetic pipes instead of the special-function unit: 2^round(x) by the exponent field, 2^f
-// for the remaining |f| <= 1/2 by the polynomial of degree 3 with the least relative error there (7.5e-5, from a Remez
-// iteration: an eighth of bf16's half step and a sixth of fp16's).  Below -125 it stays at 2^-125.
+// 2^x for two values at once, in the arithmetic pipes instead of the special-function unit: 2^f for the |f| <= 1/2 that rounding x
+// leaves, by the polynomial of degree 3 with the least relative error there (7.5e-5, from a Remez iteration: an eighth of bf16's
+// half step and a sixth of fp16's), times 2^round(x), put together from its exponent field.  0 below -126.5, and for -inf: what
+// is masked is nothing at all.
 __device__ __forceinline__ float2 pr_exp2_poly(float2 x) {
-    x.x = fmaxf(x.x, -125.f);
-    x.y = fmaxf(x.y, -125.f);
+    x.x = fmaxf(x.x, -127.f);
+    x.y = fmaxf(x.y, -127.f);
     const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);
     const float2 t = pr_add2(x, magic);            // the rounded value in the low bits
     const float2 n = pr_add2(t, unmagic);
@@ -117,9 +125,8 @@ __device__ __forceinline__ float2 pr_exp2_poly(float2 x) {
     float2 y = pr_fma2(f, make_float2(0.0551716685f, 0.0551716685f), make_float2(0.242611125f, 0.242611125f));
     y = pr_fma2(y, f, make_float2(0.693260968f, 0.693260968f));
     y = pr_fma2(y, f, make_float2(0.999928057f, 0.999928057f));
-    y.x = __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
-    y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
-    return y;
+    const float2 s = make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u));
+    return pr_mul2(y, s);
 }
 
 // largest magnitude bits of the two halves of each word; >= EXP in a half: that value is not finite
@@ -145,10 +152,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     constexpr int HALVES = D / 64;
     constexpr int RING = SM::RING;
     // Share of the exponentials, in eighths, that the arithmetic pipes take over from the special-function unit (16 a clock and SM:
-    // as long for a stage's exponentials as the tensor core for its products).  More of them costs more instructions and more
-    // power than the unit's relief gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128, after half a second of load: 0, 1,
-    // 2 eighths 802, 779, 774 us; 16 ragged prompts: 176, 162, 161 us; 3 eighths: 711 against 661 us before the clock falls.
-    constexpr int POLY = 2;
+    // as long for a stage's exponentials as the tensor core for its products).  More of them costs more instructions than the
+    // unit's relief gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128: 0, 1, 2, 3 eighths 679, 665, 673, 689 us; 16
+    // ragged prompts: 176, 161, 161, 176 us.
+    constexpr int POLY = 1;
     extern __shared__ __align__(1024) uint8_t pr_smem[];
     uint8_t *smem = pr_smem;
     const uint32_t base = pf_smem_u32(pr_smem);
@@ -460,13 +467,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     else s0 = pr_add2(s0, e);
                     pw[w] = pf_pack2<BF16>(e.x, e.y);
                 }
-                if (masked) {   // (the polynomial's smallest value is 2^-125: what is masked is nothing at all)
-#pragma unroll
-                    for (int w = 0; w < 32; ++w) {
-                        const int32_t more = my_pos - (t_base + 64 * h + 2 * w);
-                        pw[w] = more < 0 ? 0u : more == 0 ? pw[w] & 0xffffu : pw[w];
-                    }
-                }
                 tmem_st32(tmem_s + 32 * h, pw);   // a thread overwrites only its own row's scores, which it has read
             }
             s0 = pr_add2(s0, s1);
@@ -520,6 +520,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (ok) {
             tc_fence_after();
             const float inv = spoiled ? __int_as_float(0x7fc00000) : 1.f / l_run;
+            const bool wide_out = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;
             const bool repair = *not_finite == (uint32_t)k + 1u;
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((int64_t)(it.seq0 + my_pos) * p.n_q_heads + it.kvh * G + my_g) * D);
             const uint16_t *vrow = p.v + (int64_t)(it.seq0 + tok0 + 1) * p.v_stride + (int64_t)it.kvh * D;
@@ -538,14 +539,19 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                 if ((b & 0x7fffu) >= (BF16 ? 0x7f80u : 0x7c00u)) ov[c] = __float_as_uint(__uint_as_float(ov[c]) + x);
                             }
                     }
+                    uint32_t w[16];
 #pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
-                        uint4 v;
-                        v.x = pf_pack2<BF16>(__uint_as_float(ov[c]) * inv, __uint_as_float(ov[c + 1]) * inv);
-                        v.y = pf_pack2<BF16>(__uint_as_float(ov[c + 2]) * inv, __uint_as_float(ov[c + 3]) * inv);
-                        v.z = pf_pack2<BF16>(__uint_as_float(ov[c + 4]) * inv, __uint_as_float(ov[c + 5]) * inv);
-                        v.w = pf_pack2<BF16>(__uint_as_float(ov[c + 6]) * inv, __uint_as_float(ov[c + 7]) * inv);
-                        dst[(c0 + c) >> 3] = v;
+                    for (int c = 0; c < 16; ++c) w[c] = pf_pack2<BF16>(__uint_as_float(ov[2 * c]) * inv, __uint_as_float(ov[2 * c + 1]) * inv);
+                    // whole sectors (32 bytes) a store: the rows lie apart, and a sector written in two halves takes the way to L2 twice
+                    if (wide_out) {
+#pragma unroll
+                        for (int c = 0; c < 16; c += 8)
+                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + c0 / 8 + c / 4), "r"(w[c]), "r"(w[c + 1]),
+                                         "r"(w[c + 2]), "r"(w[c + 3]), "r"(w[c + 4]), "r"(w[c + 5]), "r"(w[c + 6]), "r"(w[c + 7])
+                                         : "memory");
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 16; c += 4) dst[c0 / 8 + c / 4] = make_uint4(w[c], w[c + 1], w[c + 2], w[c + 3]);
                     }
                 }
             }
