@@ -588,6 +588,14 @@ def test_evict_in_place_over_many_blocks():
     run_evict(4, 2, 64, BF16, [9000], 1111, 1000, 311, in_place=True)
 
 
+@pytest.mark.parametrize("in_place,fp8,alias", [(True, False, False), (False, True, True), (True, True, True), (False, False, False)])
+def test_evict_of_more_pairs_than_sms(in_place, fp8, alias):
+    """More (sequence, KV head) pairs than one wave of the selecting CTAs takes."""
+    lens = [(37 * i) % 300 for i in range(90)] + [1500]
+    run_evict(8, 4, 128, F16, lens, 90, 11, 313, fp8=fp8, in_place=in_place, alias_lens=alias)
+    run_evict(8, 8, 64 if not fp8 else 128, BF16, [700] * 40, 650, 0, 314, fp8=fp8, in_place=in_place, alias_lens=alias)
+
+
 def test_evict_with_one_of_the_two_in_place():
     run_evict(4, 2, 128, F16, [333, 20], 100, 10, 312, in_place=True, w_in_place=False)
     run_evict(4, 2, 128, F16, [333, 20], 100, 10, 312, in_place=False, w_in_place=True)
