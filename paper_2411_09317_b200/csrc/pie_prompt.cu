@@ -32,7 +32,7 @@ namespace {
 
 constexpr int PR_KV = 128;                    // tokens of a stage
 constexpr int PR_SOFTMAX_THREADS = 256;       // warps 0 .. 3: tile 0, warps 4 .. 7: tile 1
-constexpr int PR_THREADS = PR_SOFTMAX_THREADS + 128;  // + the issuing warp (8), the loading warp (9) and two that only give registers
+constexpr int PR_THREADS = PR_SOFTMAX_THREADS + 128;  // + the issuing warp (8), the loading warp (9) and two that look V over (10, 11)
 // Registers: 384 threads get 168 each at launch; the softmax warpgroups, whose threads hold a row of 128 scores, take over what
 // the third gives up: 2 x 128 x 208 + 128 x 88 = 384 x 168.
 constexpr int PR_REGS_SOFTMAX = 208, PR_REGS_REST = 88;
@@ -64,8 +64,8 @@ struct PrSmem {
     static constexpr int RING = D == 128 ? 5 : 8;
     static constexpr int OFF_Q = 0;
     static constexpr int OFF_RING = OFF_Q + Q_BYTES;
-    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], free[4], s[2], p[2], done[2], q[2], k0
-    static constexpr int OFF_MISC = OFF_BAR + 18 * 8;         // [0] TMEM base, [1] abort, [4 .. 7] items in which a value was not finite
+    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], clean[4], free[4], s[2], p[2], done[2], q[2], k0
+    static constexpr int OFF_MISC = OFF_BAR + 22 * 8;         // [0] TMEM base, [1] abort, [4 .. 7] items in which a value was not finite
     static constexpr int BYTES = OFF_MISC + 32;
 };
 
@@ -165,10 +165,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         return;
     }
     // A CTA works through its items without a break: the stages of all of them form one sequence g = 0, 1, ...  Ring entry 2 g
-    // is K, 2 g + 1 is V of stage g.  full[g & 3]: V(g) and K(g + 1) have landed.  free[f & 3]: f = 0: the first scores, f = g + 1:
+    // is K, 2 g + 1 is V of stage g.  full[g & 3]: V(g) and K(g + 1) have landed; clean[g & 3]: and V(g) may be multiplied.  free[f & 3]: f = 0: the first scores, f = g + 1:
     // all MMAs of stage g (O += P V of both tiles and the next scores) are complete.  Per tile: s: scores complete, p: P in place,
     // done: O of the item complete, q: its query rows have landed.
-    const uint32_t bar_full = base + SM::OFF_BAR, bar_free = bar_full + 32, bar_s = bar_free + 32, bar_p = bar_s + 16, bar_done = bar_p + 16;
+    const uint32_t bar_full = base + SM::OFF_BAR, bar_clean = bar_full + 32, bar_free = bar_clean + 32, bar_s = bar_free + 32, bar_p = bar_s + 16, bar_done = bar_p + 16;
     const uint32_t bar_q = bar_done + 16, bar_k0 = bar_q + 16;
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
 
@@ -197,6 +197,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     if (tid == 0) {
         for (int i = 0; i < 4; ++i) {
             pf_mbar_init(bar_full + 8 * i, 1);
+            pf_mbar_init(bar_clean + 8 * i, 2);   // warps 10 and 11
             pf_mbar_init(bar_free + 8 * i, 1);
             misc[4 + i] = 0;
         }
@@ -362,7 +363,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const uint32_t k_slot = v_slot + 1 == RING ? 0 : v_slot + 1;
                 const uint64_t vd = v_desc + (uint64_t)(v_slot * (SM::STAGE >> 4));
                 const bool last = j + 1 == it.n;
-                ok = wait_all(bar_full + 8 * (g & 3), (uint32_t)((g >> 2) & 1));   // V(g) and K(g + 1) have landed
+                ok = wait_all(bar_clean + 8 * (g & 3), (uint32_t)((g >> 2) & 1));   // V(g) and K(g + 1) are there
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int32_t n = t == 0 ? it.n0 : it.n1, nx = t == 0 ? nx0 : nx1;
@@ -394,6 +395,53 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             it = next;
         }
         __syncwarp();
+    } else {
+        // =============================================================================== the warps that look V over
+        // Values that some row of the item may not see meet P = 0 there, which hides everything but NaN and infinities.  Those
+        // are cleared in the stage and, if there were any, added at the end to the rows that do see them.  (Done by the softmax
+        // warps in front of their arrival it took 1000 to 1700 cycles of every masked stage.)
+        Item it, next;
+        bool more = get_item(0, it), ok = true;
+        const int me = (warp - 10) * 32 + lane;
+        int32_t g = 0;
+        for (int32_t k = 0; more && ok; ++k) {
+            more = get_item(k + 1, next);
+            for (int32_t j = 0; j < it.n; ++j, ++g) {
+                ok = wait_all(bar_full + 8 * (g & 3), (uint32_t)((g >> 2) & 1));
+                if (!ok) break;
+                const int32_t first = it.tok0 + 1 - j * PR_KV;   // rows of the stage from here on are masked for some row of the item
+                if (first < PR_KV) {
+                    uint8_t *vs = smem + SM::OFF_RING + (2 * g + 1) % RING * SM::STAGE;
+                    bool found = false;
+                    for (int e = max(0, first) * 8 + me; e < PR_KV * 8; e += 256) {
+                        uint4 w[4][HALVES];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int h = 0; h < HALVES; ++h)
+                                w[u][h] = e + 64 * u < PR_KV * 8 ? *reinterpret_cast<const uint4 *>(vs + h * (PR_KV * 128) + (e + 64 * u) * 16) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int h = 0; h < HALVES; ++h)
+                                if (pr_not_finite<BF16>(w[u][h])) {
+                                    found = true;
+                                    *reinterpret_cast<uint4 *>(vs + h * (PR_KV * 128) + (e + 64 * u) * 16) =
+                                        make_uint4(pr_clear_not_finite<BF16>(w[u][h].x), pr_clear_not_finite<BF16>(w[u][h].y),
+                                                   pr_clear_not_finite<BF16>(w[u][h].z), pr_clear_not_finite<BF16>(w[u][h].w));
+                                }
+                    }
+                    if (found) {
+                        misc[4 + (k & 3)] = (uint32_t)k + 1u;
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) pf_mbar_arrive(bar_clean + 8 * (g & 3));
+            }
+            it = next;
+        }
+        __syncwarp();
     }
     } else {
         // =============================================================================== the softmax warps
@@ -406,16 +454,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         Item it, next;
         bool more = get_item(0, it), ok = true;
         uint32_t s_count = 0, done_count = 0;
-        int32_t g0 = 0;   // the item's first stage
-        for (int32_t k = 0; more && ok; ++k, g0 += it.n, it = next) {
+        for (int32_t k = 0; more && ok; ++k, it = next) {
         more = get_item(k + 1, next);
         const int32_t n = t == 0 ? it.n0 : it.n1, tok0 = it.tok0;
         if (n == 0) continue;
         const int32_t first = tok0 + t * TT;                          // the tile's first position
         const int32_t my_pos = first + my_tok;
         const bool row_valid = my_tok < TT && my_pos < it.len;
-        volatile uint32_t *not_finite = misc + 4 + (k & 3);
-        float m_run = -INFINITY, l_run = 0.f;
+                float m_run = -INFINITY, l_run = 0.f;
         bool spoiled = false;                                         // a score the row sees is NaN or +inf: so is the softmax
         for (int32_t j = 0; j < n; ++j) {
             if (!wait_all(bar_s + 8 * t, s_count & 1u)) { ok = false; break; }
@@ -483,31 +529,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     tmem_st32(tmem_o + c0, ov);
                 }
             }
-            if (masked) {
-                // Values that some row of the item may not see meet P = 0 there, which hides everything but NaN and infinities.
-                // Those are cleared in the stage and, if there were any, added at the end to the rows that do see them.
-                const int32_t g = g0 + j;
-                if (!wait_all(bar_full + 8 * (g & 3), (uint32_t)((g >> 2) & 1))) { ok = false; break; }
-                uint8_t *vs = smem + SM::OFF_RING + (2 * g + 1) % RING * SM::STAGE;
-                const int row_first = max(0, tok0 + 1 - t_base);
-                bool found = false;
-                for (int e = row_first * 8 + r; e < PR_KV * 8; e += 128)
-#pragma unroll
-                    for (int h = 0; h < HALVES; ++h) {
-                        uint4 *at = reinterpret_cast<uint4 *>(vs + h * (PR_KV * 128) + e * 16);
-                        uint4 w = *at;
-                        if (pr_not_finite<BF16>(w)) {
-                            found = true;
-                            w.x = pr_clear_not_finite<BF16>(w.x);
-                            w.y = pr_clear_not_finite<BF16>(w.y);
-                            w.z = pr_clear_not_finite<BF16>(w.z);
-                            w.w = pr_clear_not_finite<BF16>(w.w);
-                            *at = w;
-                        }
-                    }
-                if (found) *not_finite = (uint32_t)k + 1u;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -521,7 +542,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             tc_fence_after();
             const float inv = spoiled ? __int_as_float(0x7fc00000) : 1.f / l_run;
             const bool wide_out = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;
-            const bool repair = *not_finite == (uint32_t)k + 1u;
+            const bool repair = misc[4 + (k & 3)] == (uint32_t)k + 1u;
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((int64_t)(it.seq0 + my_pos) * p.n_q_heads + it.kvh * G + my_g) * D);
             const uint16_t *vrow = p.v + (int64_t)(it.seq0 + tok0 + 1) * p.v_stride + (int64_t)it.kvh * D;
 #pragma unroll 1
