@@ -8,6 +8,7 @@
 // and the cache rows they lie in.  evict_move_kernel copies the rows; it is a programmatic dependent of the first.
 // Bound: bytes (kept rows in and out; the weights once).
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/pie.h"
 #include "pie_kernels.h"
@@ -49,6 +50,21 @@ __device__ __forceinline__ int32_t unit_slot(const EvictParams &p, const int32_t
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// Of 16 words in shared memory, one per warp: the sum of those in front of this warp's, and of all.
+__device__ __forceinline__ uint32_t warps_before(const int32_t *sums, uint32_t *all) {
+    static_assert(SEL_WARPS == 16, "");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t mine = lane < SEL_WARPS ? (uint32_t)sums[lane] : 0u;
+    uint32_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < SEL_WARPS; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    *all = __shfl_sync(0xffffffffu, inc, SEL_WARPS - 1);
+    return __shfl_sync(0xffffffffu, inc - mine, warp);
+}
+
 // The bin (counted from the top) in which the count from above reaches *rank; *rank becomes the rank inside it.  BINS
 // counters in shared memory, read by every thread of the CTA.  Three barriers.
 template <int BINS>
@@ -74,9 +90,8 @@ __device__ __forceinline__ uint32_t find_bin(const int32_t *hist, int32_t *rank,
     }
     if (lane == 31) warp_sums[warp] = inc;
     __syncthreads();
-    int32_t above = inc - mine;
-#pragma unroll
-    for (int w = 0; w < SEL_WARPS; ++w) above += w < warp ? warp_sums[w] : 0;
+    uint32_t all;
+    int32_t above = inc - mine + (int32_t)warps_before(warp_sums, &all);
     const int32_t want = *rank;
     if (above < want && want <= above + mine) {
 #pragma unroll
@@ -125,8 +140,8 @@ evict_select_kernel(const EvictParams p, int32_t smem_slots) {
     uint32_t wt[ITEMS];
     auto token = [&](int32_t base, int i) { return base + tid * ITEMS + i; };
     const bool aligned = ITEMS % 4 == 0 && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
-    auto read_piece = [&](int32_t base) {
-        if (aligned && token(base, ITEMS) <= ctx) {
+    auto read_piece = [&](int32_t base, int64_t end) {
+        if (aligned && token(base, ITEMS) <= end) {
 #pragma unroll
             for (int i = 0; i + 3 < ITEMS; i += 4) {
                 const uint4 v = *reinterpret_cast<const uint4 *>(w + token(base, i));
@@ -134,13 +149,15 @@ evict_select_kernel(const EvictParams p, int32_t smem_slots) {
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) wt[i] = token(base, i) < ctx ? w[token(base, i)] : 0u;
+            for (int i = 0; i < ITEMS; ++i) wt[i] = token(base, i) < end ? w[token(base, i)] : 0u;
         }
     };
+    // of the thread's items, those below a token number, as bits
+    auto below = [&](int32_t base, int32_t end) { return (1u << max(0, min(ITEMS, end - token(base, 0)))) - 1u; };
+    read_piece(0, a.weights_stride);   // (on its way before the length is known; what lies behind it is not looked at)
     const bool one_piece = ctx <= PIECE;
     bool missing = false;
     if (fits) {
-        if (one_piece) read_piece(0);
         for (int32_t i = tid; i < (ctx + 15) / 16; i += SEL_THREADS) {
             const int32_t slot = unit_slot(p, src_row, i);
             if (smem_slots) slots[i] = slot;
@@ -151,7 +168,12 @@ evict_select_kernel(const EvictParams p, int32_t smem_slots) {
     }
     for (int i = tid; i < SEL_BINS / 4; i += SEL_THREADS) reinterpret_cast<int4 *>(hist)[i] = make_int4(0, 0, 0, 0);
     if (tid == 0) n_list = 0;
+    // Weights that are all positive numbers (or 0 or infinity) are in order as they are: the usual case, and a third fewer instructions
+    bool odd = !one_piece;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) odd |= token(0, i) < ctx && wt[i] > 0x7f800000u;
     missing = __syncthreads_or(missing) != 0;
+    const bool plain = __syncthreads_or(odd) == 0;
     if (!fits || missing) {
         if (tid == 0) {
             *reinterpret_cast<volatile int32_t *>(a.status + (fits ? 0 : 1)) = 1;
@@ -167,117 +189,124 @@ evict_select_kernel(const EvictParams p, int32_t smem_slots) {
     const int32_t n_old = ctx - min(ctx, a.recent);              // the tokens that compete
     const int32_t places = ctx > a.budget ? a.budget - a.recent : n_old;
     const bool all_old = places >= n_old;
-    uint32_t edge = 0xffffffffu;                                 // keys above it stay (no weight has this pattern's key: a NaN)
-    int32_t n_edge = 0;                                          // and this many of those equal to it
-    if (!all_old && places > 0) {
-        int32_t rank = places;                                   // the edge is the rank-th largest of those that share its digits so far
-        edge = 0;
-        auto count = [&](uint32_t known, int shift, uint32_t digit_mask) {
+    auto work = [&](auto plain_tag) {
+        auto key = [](uint32_t b) { return decltype(plain_tag)::value ? b | 0x80000000u : weight_key(b); };
+        uint32_t edge = 0xffffffffu;                                 // keys above it stay (no weight has this pattern's key: a NaN)
+        int32_t n_edge = 0;                                          // and this many of those equal to it
+        if (!all_old && places > 0) {
+            int32_t rank = places;                                   // the edge is the rank-th largest of those that share its digits so far
+            edge = 0;
+            auto count = [&](uint32_t known, int shift, uint32_t digit_mask) {
+                for (int32_t base = 0; base < n_old; base += PIECE) {
+                    if (!one_piece) read_piece(base, ctx);
+#pragma unroll
+                    for (int i = 0; i < ITEMS; ++i) {
+                        const uint32_t k = key(wt[i]);
+                        if (token(base, i) < n_old && (k & known) == edge) atomicAdd(&hist[(k >> shift) & digit_mask], 1);
+                    }
+                }
+                __syncthreads();
+            };
+            auto clear = [&]() {
+                for (int i = tid; i < 1024; i += SEL_THREADS) hist[i] = 0;
+                __syncthreads();
+            };
+            count(0u, 20, 0xfffu);
+            edge |= find_bin<SEL_BINS>(hist, &rank, warp_sums, answer) << 20;
+            // the candidates: the weights with that digit
             for (int32_t base = 0; base < n_old; base += PIECE) {
-                if (!one_piece) read_piece(base);
+                if (!one_piece) read_piece(base, ctx);
 #pragma unroll
                 for (int i = 0; i < ITEMS; ++i) {
-                    const uint32_t k = weight_key(wt[i]);
-                    if (token(base, i) < n_old && (k & known) == edge) atomicAdd(&hist[(k >> shift) & digit_mask], 1);
+                    const uint32_t k = key(wt[i]);
+                    if (token(base, i) < n_old && (k & 0xfff00000u) == edge) {
+                        const int32_t at = atomicAdd(&n_list, 1);
+                        if (at < SEL_LIST) list[at] = k;
+                    }
                 }
             }
             __syncthreads();
-        };
-        auto clear = [&]() {
-            for (int i = tid; i < 1024; i += SEL_THREADS) hist[i] = 0;
-            __syncthreads();
-        };
-        count(0u, 20, 0xfffu);
-        edge |= find_bin<SEL_BINS>(hist, &rank, warp_sums, answer) << 20;
-        // the candidates: the weights with that digit
-        for (int32_t base = 0; base < n_old; base += PIECE) {
-            if (!one_piece) read_piece(base);
+            const int32_t m = n_list;
+            if (m <= SEL_LIST) {
+                // the rank-th largest: every candidate counts those above it and those like it (whatever their order in the list)
+                if (tid < m) {
+                    const uint32_t k = list[tid];
+                    int32_t above = 0, like = 0;
+#pragma unroll 8
+                    for (int32_t i = 0; i < m; ++i) {
+                        above += list[i] > k;
+                        like += list[i] == k;
+                    }
+                    if (above < rank && rank <= above + like) {   // (all candidates like the answer write the same)
+                        answer[0] = (int32_t)k;
+                        answer[1] = rank - above;
+                    }
+                }
+                __syncthreads();
+                edge = (uint32_t)answer[0];
+                rank = answer[1];
+            } else {
+                clear();
+                count(0xfff00000u, 10, 0x3ffu);
+                edge |= find_bin<1024>(hist, &rank, warp_sums, answer) << 10;
+                clear();
+                count(0xfffffc00u, 0, 0x3ffu);
+                edge |= find_bin<1024>(hist, &rank, warp_sums, answer);
+            }
+            n_edge = rank;
+        }
+
+        // ---- in order: the kept positions, where their rows lie, their weights.  Of the first x tokens above(x) + min(on_edge(x),
+        // n_edge) stay, so both counts can be summed up before any token's fate is known.
+        int32_t above_before = 0, edge_before = 0;
+        for (int32_t base = 0; base < ctx; base += PIECE) {
+            if (!one_piece) read_piece(base, ctx);
+            uint32_t larger = 0, like = 0;                           // a bit per item
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                const uint32_t k = weight_key(wt[i]);
-                if (token(base, i) < n_old && (k & 0xfff00000u) == edge) {
-                    const int32_t at = atomicAdd(&n_list, 1);
-                    if (at < SEL_LIST) list[at] = k;
-                }
+                const uint32_t k = key(wt[i]);
+                larger |= (uint32_t)(k > edge) << i;
+                like |= (uint32_t)(k == edge) << i;
             }
-        }
-        __syncthreads();
-        const int32_t m = n_list;
-        if (m <= SEL_LIST) {
-            // the rank-th largest: every candidate counts those above it and those like it (whatever their order in the list)
-            if (tid < m) {
-                const uint32_t k = list[tid];
-                int32_t above = 0, like = 0;
-                for (int32_t i = 0; i < m; ++i) {
-                    above += list[i] > k;
-                    like += list[i] == k;
-                }
-                if (above < rank && rank <= above + like) {   // (all candidates like the answer write the same)
-                    answer[0] = (int32_t)k;
-                    answer[1] = rank - above;
-                }
+            const uint32_t in_ctx = below(base, ctx), old = below(base, n_old);
+            const uint32_t is_above = in_ctx & (all_old ? ~0u : ~old | larger);
+            uint32_t is_edge = all_old ? 0u : old & like;
+            // both counts in one word: a piece has at most 2^13 tokens
+            const uint32_t mine = (uint32_t)__popc(is_above) | (uint32_t)__popc(is_edge) << 16;
+            uint32_t inc = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += y;
             }
-            __syncthreads();
-            edge = (uint32_t)answer[0];
-            rank = answer[1];
-        } else {
-            clear();
-            count(0xfff00000u, 10, 0x3ffu);
-            edge |= find_bin<1024>(hist, &rank, warp_sums, answer) << 10;
-            clear();
-            count(0xfffffc00u, 0, 0x3ffu);
-            edge |= find_bin<1024>(hist, &rank, warp_sums, answer);
-        }
-        n_edge = rank;
-    }
-
-    // ---- in order: the kept positions, where their rows lie, their weights.  Of the first x tokens above(x) + min(on_edge(x),
-    // n_edge) stay, so both counts can be summed up before any token's fate is known.
-    int32_t above_before = 0, edge_before = 0;
-    for (int32_t base = 0; base < ctx; base += PIECE) {
-        if (!one_piece) read_piece(base);
-        uint32_t is_above = 0, is_edge = 0;                      // a bit per item
+            if (lane == 31) warp_sums[warp] = (int32_t)inc;
+            __syncthreads();                                         // (every weight of the piece is read: in place, writing may begin)
+            uint32_t all;
+            const uint32_t before = inc - mine + warps_before(warp_sums, &all);
+            const int32_t on_edge = edge_before + (int32_t)(before >> 16);
+            int32_t j = above_before + (int32_t)(before & 0xffffu) + min(on_edge, n_edge);
+            above_before += (int32_t)(all & 0xffffu);
+            edge_before += (int32_t)(all >> 16);
+            const int32_t left = max(0, n_edge - on_edge);           // of the thread's on the edge, so many stay: the first ones
+            while (__popc(is_edge) > left) is_edge &= ~(1u << (31 - __clz(is_edge)));
+            const uint32_t keep = is_above | is_edge;
+            if (keep) {
+                const int32_t t0 = token(base, 0);                   // (the thread's items lie in one block)
+                const int32_t row0 = (smem_slots ? slots[t0 >> 4] : unit_slot(p, src_row, t0 >> 4)) * 16 + (t0 & 15);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int32_t t = token(base, i);
-            const uint32_t k = weight_key(wt[i]);
-            is_above |= (uint32_t)(t < ctx && (t >= n_old || all_old || k > edge)) << i;
-            is_edge |= (uint32_t)(t < n_old && !all_old && k == edge) << i;
-        }
-        // both counts in one word: a piece has at most 2^13 tokens
-        const uint32_t mine = (uint32_t)__popc(is_above) | (uint32_t)__popc(is_edge) << 16;
-        uint32_t inc = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += y;
-        }
-        if (lane == 31) warp_sums[warp] = (int32_t)inc;
-        __syncthreads();                                         // (every weight of the piece is read: in place, writing may begin)
-        uint32_t before = inc - mine, all = 0;
-#pragma unroll
-        for (int v = 0; v < SEL_WARPS; ++v) {
-            const uint32_t x = (uint32_t)warp_sums[v];
-            before += v < warp ? x : 0u;
-            all += x;
-        }
-        int32_t above = above_before + (int32_t)(before & 0xffffu), on_edge = edge_before + (int32_t)(before >> 16);
-        above_before += (int32_t)(all & 0xffffu);
-        edge_before += (int32_t)(all >> 16);
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const bool a_i = (is_above >> i) & 1u, e_i = (is_edge >> i) & 1u;
-            const int32_t j = above + min(on_edge, n_edge), t = token(base, i);
-            if ((a_i || (e_i && on_edge < n_edge)) && j < n_new) {
-                if (kept != nullptr) kept[j] = t;
-                rows[j] = (smem_slots ? slots[t >> 4] : unit_slot(p, src_row, t >> 4)) * 16 + (t & 15);
-                w_out[j] = wt[i];                                // j <= t: in place this overwrites only what has been read
+                for (int i = 0; i < ITEMS; ++i)
+                    if (((keep >> i) & 1u) && j < n_new) {
+                        if (kept != nullptr) kept[j] = t0 + i;
+                        rows[j] = row0 + i;
+                        w_out[j] = wt[i];                            // j <= t: in place this overwrites only what has been read
+                        ++j;
+                    }
             }
-            above += a_i;
-            on_edge += e_i;
+            if (!one_piece) __syncthreads();                         // (the counts have been read)
         }
-        if (!one_piece) __syncthreads();                         // (the counts have been read)
-    }
+    };
+    if (plain) work(std::true_type());
+    else work(std::false_type());
     for (int64_t t = n_new + tid; t < min((int64_t)ctx, a.weights_out_stride); t += SEL_THREADS) w_out[t] = 0u;
     if (kept != nullptr)
         for (int32_t j = n_new + tid; j < a.budget; j += SEL_THREADS) kept[j] = -1;
