@@ -381,8 +381,8 @@ int pie_rope_plan(int32_t head_dim, int32_t rotary_dim, const int32_t *pair_axis
  * A token whose block is not on the GPU, or whose sequence or position is out of range, is rotated but not written, and the
  * next call that checks the device status word returns PIE_ERR_NOT_RESIDENT / PIE_ERR_INVALID.  Two tokens of one call must
  * not name the same place.  Enqueued and ordered like pie_kv_write; one token per sequence is the decode step's form.
- * PIE_ERR_INVALID: before pie_set_rope, a pointer or stride not on a 16-byte boundary, a stride below its row, an output that
- * overlaps an input otherwise than named above.  PIE_ERR_UNSUPPORTED while the compute stream is being captured: calls on a
+ * PIE_ERR_INVALID: before pie_set_rope, a pointer or stride not on a 16-byte boundary (the int32 arrays: a 4-byte one), a stride
+ * below its row, an output that overlaps an input otherwise than named above.  PIE_ERR_UNSUPPORTED while the compute stream is being captured: calls on a
  * pool keep host-side books, which a replayed graph would not. */
 int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out, const void *k, void *k_out, const void *v,
                       const int32_t *positions_dev, const int32_t *token_seq_dev, const int32_t *token_pos_dev,
@@ -398,11 +398,12 @@ int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out,
  * pools too: the arrays are 16-bit), tokens q_stride / k_stride / v_stride elements apart (0: dense); out: dense, like q.
  * Sequences of any length, empty ones too; rows behind the last offset are left as they were.  What a token may not see
  * cannot reach it, NaN and infinities included.  Scores and sums in fp32, probabilities rounded to the 16-bit type before
- * they meet the values (each by 2^-9 (bf16) or 2^-12 (fp16) of itself at most, independently: less than the output's own
- * rounding), out rounded to nearest.
- * offsets_host: host, n_seqs + 1 entries, first 0, ascending.  PIE_ERR_INVALID: offsets that are not, pointers or strides not
- * on a 16-byte boundary, a stride below its row, out overlapping an input.  PIE_ERR_UNSUPPORTED while the compute stream is
- * being captured. */
+ * they meet the values (each by half a step of itself at most, 2^-8 (bf16) or 2^-11 (fp16), independently of the others),
+ * exponentials to 1e-4, out rounded to nearest.
+ * offsets_host: host, n_seqs + 1 entries, first 0, ascending; read before the call returns.  PIE_ERR_INVALID: offsets that are
+ * not, pointers or strides not on a 16-byte boundary, a stride below its row, out overlapping an input, more than 131072 pieces
+ * of 256 / (n_q_heads / n_kv_heads) tokens (counted per sequence) in one call of a small pool.  PIE_ERR_UNSUPPORTED while the
+ * compute stream is being captured. */
 int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const void *v, void *out, const int32_t *offsets_host,
                          int32_t n_seqs, float scale, int64_t q_stride, int64_t k_stride, int64_t v_stride);
 /* The host half of pie_prompt_attention by itself (needs no GPU): checks the offsets and cuts the sequences into items of
@@ -448,7 +449,8 @@ int pie_decode_attention_weights(pie_pool *pool, int32_t layer, const void *q, v
  * With kept host copies every block of the layer counts as written.  Once all layers have evicted, the blocks behind the new
  * length can be given back (pie_block_free).
  * PIE_ERR_INVALID: budget < 1, recent < 0 or > budget, strides or widths that are not positive, a destination table
- * that is the source's own array, weights_out == weights with another stride.  PIE_ERR_UNSUPPORTED while the compute stream is being captured. */
+ * that is the source's own array, weights_out == weights with another stride, weights_out overlapping weights otherwise, an array
+ * not on a 4-byte boundary.  PIE_ERR_UNSUPPORTED while the compute stream is being captured. */
 int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, int32_t max_blocks_per_seq,
                  const int32_t *ctx_lens_dev, int32_t n_seqs, float *weights, int64_t weights_stride, int32_t budget,
                  int32_t recent, const int32_t *dst_block_table_dev, int32_t dst_max_blocks, float *weights_out,

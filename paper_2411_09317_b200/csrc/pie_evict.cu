@@ -4,9 +4,12 @@
 // Two kernels.  evict_select_kernel, one CTA per (sequence, KV head): the weight of the last token that still gets a place is
 // found digit by digit (radix select over the weights' order-preserving bit patterns, 12 + 10 + 10 bits: exact, whatever their
 // distribution, where a sort would move every weight several times).  The weights are read once into registers; the few that
-// share the first digit are ranked among themselves by comparison where they fit a list.  Then one pass in token order writes the kept positions, their weights
-// and the cache rows they lie in.  evict_move_kernel copies the rows; it is a programmatic dependent of the first.
-// Bound: bytes (kept rows in and out; the weights once).
+// share the first digit are ranked among themselves by comparison where they fit a list.  Then one pass in token order writes the
+// kept positions, their weights and the cache rows they lie in.  evict_copy_kernel (out of place) or evict_move_kernel (in place)
+// moves the rows; it is a programmatic dependent of the first.  (Both in one CTA: 264 us against 246 for 32 x 32 pairs, 41 against
+// 34 for 24 x 8: the selecting CTAs' shared memory and barriers leave too few copies in flight.)
+// Bound: bytes (kept rows in and out; the weights once): 1.1 GB in 225 us, 76 % of a plain copy's rate; rows of 256 bytes lie
+// scattered, and 30 us of it are the selection, which the first rows wait for.
 #include <algorithm>
 #include <type_traits>
 
@@ -130,13 +133,13 @@ evict_select_kernel(const EvictParams p, int32_t smem_slots) {
     const int32_t *dst_row = a.dst_table != nullptr ? a.dst_table + (int64_t)s * a.dst_max_blocks : src_row;
     const int32_t dst_blocks = a.dst_table != nullptr ? a.dst_max_blocks : a.max_blocks;
     int32_t *kept = a.kept != nullptr ? a.kept + (int64_t)pair * a.budget : nullptr;
-    int32_t *rows = a.rows + (int64_t)pair * a.budget;
+    int32_t *rows = a.rows + (int64_t)pair * a.rows_stride;
     const uint32_t *w = reinterpret_cast<const uint32_t *>(a.weights) + (int64_t)pair * a.weights_stride;
     uint32_t *w_out = reinterpret_cast<uint32_t *>(a.weights_out) + (int64_t)pair * a.weights_out_stride;
     grid_launch();
     // ---- does the sequence fit, and is everything it needs on the GPU?  (The same answer for every head of the sequence.)
-    const bool fits = ctx >= 0 && (ctx + 15) / 16 <= a.max_blocks && ctx <= a.weights_stride && n_new <= a.weights_out_stride &&
-                      (n_new + 15) / 16 <= dst_blocks;
+    const bool fits = ctx >= 0 && ctx <= (int64_t)a.max_blocks * 16 && ctx <= a.weights_stride && n_new <= a.weights_out_stride &&
+                      n_new <= (int64_t)dst_blocks * 16;
     uint32_t wt[ITEMS];
     auto token = [&](int32_t base, int i) { return base + tid * ITEMS + i; };
     const bool aligned = ITEMS % 4 == 0 && (reinterpret_cast<uintptr_t>(w) & 15) == 0;
@@ -339,7 +342,7 @@ evict_copy_kernel(const EvictParams p, int32_t chunks) {
     grid_wait();
     const int32_t n = a.counts[pair];
     if (tid < MOVE_ROWS) {   // (beyond the count: stale, not used; its load goes out beside the count's)
-        from[tid] = j0 + tid < a.budget ? a.rows[(int64_t)pair * a.budget + j0 + tid] : 0;
+        from[tid] = j0 + tid < a.rows_stride ? a.rows[(int64_t)pair * a.rows_stride + j0 + tid] : 0;
         to[tid] = dst;
     }
     if (j0 == 0 && tid == 0) write_new_len(p, pair, n);
@@ -382,7 +385,7 @@ evict_move_kernel(const EvictParams p, int32_t slice_vecs) {
     const int32_t slices = p.row_vecs / slice_vecs;
     const int32_t kv = blockIdx.y / slices, col0 = (blockIdx.y - kv * slices) * slice_vecs;
     const int32_t *table_row = a.block_table + (int64_t)s * a.max_blocks;
-    const int32_t *rows = a.rows + (int64_t)pair * a.budget;
+    const int32_t *rows = a.rows + (int64_t)pair * a.rows_stride;
     uint4 *pool = reinterpret_cast<uint4 *>(a.gpu_pool);
     const int32_t lane_col = tid % slice_vecs, lane_row = tid / slice_vecs, rows_per_pass = MOVE_THREADS / slice_vecs;
     const int32_t batch = rows_per_pass * MOVE_DEPTH;

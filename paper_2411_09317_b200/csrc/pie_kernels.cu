@@ -486,7 +486,7 @@ struct AttnParams {
     float out_scale = 1.f;  // 8-bit pools: the value scale (times what the kernel's 16-bit images of the bytes leave out)
     float k_scale = 1.f, v_scale = 1.f;  // 8-bit pools: the append stores E4M3(x / scale)
     // Calls that accumulate attention weights (instantiations with SCORES): every valid token's scores, in log2 units, as
-    // [item][token of the chunk][head of the group] - see attn_weights_kernel.
+    // [item][token of the chunk][head of the group] - see attn_finish_kernel.
     float *scores = nullptr;
 };
 

@@ -42,8 +42,6 @@ cudaError_t launch_kv_write8(const void *k, const void *v, const int32_t *token_
                              float k_scale, float v_scale, int32_t *status, cudaStream_t stream);
 
 // ---- attention -----------------------------------------------------------------------------------
-constexpr int ROPE_PAIRS = 64;  // head_dim / 2 at most
-
 struct AttnShape {
     int head_dim;      // 64 or 128
     int dtype;         // PIE_F16 / PIE_BF16
@@ -54,6 +52,7 @@ struct AttnShape {
 };
 
 // ---- rotary positions, fused with the cache write ---------------------------------------------------
+constexpr int ROPE_PAIRS = 64;  // head_dim / 2 at most
 struct RopeTable {
     uint64_t turns[ROPE_PAIRS];  // 2^64-ths of a turn per position
     uint8_t axis[ROPE_PAIRS];    // which row of the positions turns the pair
@@ -100,10 +99,11 @@ struct EvictLaunch {
     float *weights_out;
     int64_t weights_stride, weights_out_stride;
     int32_t *new_lens, *kept;    // may be NULL
-    int32_t *rows;               // scratch [n_seqs * n_kv_heads][budget]: slot * 16 + row of each kept token
+    int32_t *rows;               // scratch [n_seqs * n_kv_heads][rows_stride]: slot * 16 + row of each kept token
     int32_t *counts;             // scratch [n_seqs * n_kv_heads]: kept tokens, -1: the sequence is left alone
     void *gpu_pool;
     int32_t max_blocks, dst_max_blocks, n_seqs, budget, recent;
+    int32_t rows_stride;         // what a sequence can keep at most
     int32_t *status;
 };
 cudaError_t evict_configure();
@@ -159,7 +159,7 @@ struct AttnLaunch {
     void *prev_out = nullptr;
     int parity = 0;
     // Accumulated attention weights: device fp32 [n_seqs][n_kv_heads][weights_stride], or NULL.  The kernel then leaves every
-    // score in the scratch, and one more kernel turns them into weights (variant 0 only; not deferred).
+    // score in the scratch, and the kernel that merges the chunks turns them into weights (the default variant's shape; not deferred).
     float *weights = nullptr;
     int64_t weights_stride = 0;
 };

@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstring>
 #include <deque>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -1236,13 +1237,20 @@ struct OnDevice {
 struct Rows {
     const void *p;
     int64_t n, row, stride;
-    bool aligned() const { return !p || (((uintptr_t)p & 15) == 0 && stride % 8 == 0 && stride >= row); }
+    bool aligned() const { return !p || (((uintptr_t)p & 15) == 0 && stride % 8 == 0 && stride >= row && stride <= (1ll << 36)); }
     bool overlaps(const Rows &o) const {
         if (!p || !o.p || n <= 0 || o.n <= 0) return false;
         const uintptr_t a = (uintptr_t)p, b = (uintptr_t)o.p;
         return a < b + (uintptr_t)((o.n - 1) * o.stride + o.row) * 2 && b < a + (uintptr_t)((n - 1) * stride + row) * 2;
     }
 };
+
+// arrays of 32-bit words: NULL or on a word's boundary
+bool words_aligned(std::initializer_list<const void *> arrays) {
+    for (const void *a : arrays)
+        if ((uintptr_t)a & 3) return false;
+    return true;
+}
 
 // is the compute stream being captured into a graph?  (A replay would pass the host's books by.)
 bool capturing(pie_pool *p) {
@@ -2124,6 +2132,7 @@ int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out,
     if (k_stride == 0) k_stride = kv_row;
     if (v_stride == 0) v_stride = kv_row;
     if (write && (max_blocks_per_seq <= 0 || n_seqs <= 0)) return PIE_ERR_INVALID;
+    if (!words_aligned({positions_dev, token_seq_dev, token_pos_dev, block_table_dev})) return PIE_ERR_INVALID;
     if (n_tokens > 0) {
         if (!positions_dev || (!q && !k) || (q != nullptr) != (q_out != nullptr) || (!k && k_out)) return PIE_ERR_INVALID;
         if (write && (!k || !v || !token_seq_dev || !token_pos_dev)) return PIE_ERR_INVALID;
@@ -2258,7 +2267,7 @@ int pie_decode_attention_weights(pie_pool *pool, int32_t layer, const void *q, v
                                  int32_t max_blocks_per_seq, const int32_t *ctx_lens_dev, const int32_t *block_table_host,
                                  const int32_t *ctx_lens_host, int32_t n_seqs, float scale, const void *k_new,
                                  const void *v_new, float *weights, int64_t weights_stride) {
-    if (!pool || !weights || weights_stride <= 0 || ((uintptr_t)weights & 3)) return PIE_ERR_INVALID;
+    if (!pool || !weights || weights_stride <= 0 || !words_aligned({weights, block_table_dev, ctx_lens_dev})) return PIE_ERR_INVALID;
     if (pool->sticky != PIE_OK) return pool->sticky;
     OnDevice on(pool->device);
     if (capturing(pool)) return PIE_ERR_UNSUPPORTED;
@@ -2306,13 +2315,17 @@ int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, 
     if (layer < 0 || layer >= pool->cfg.n_layers) return PIE_ERR_RANGE;
     if (n_seqs > 0 && (!block_table_dev || !ctx_lens_dev || !weights || weights_stride <= 0)) return PIE_ERR_INVALID;
     if (dst_block_table_dev && (dst_max_blocks <= 0 || dst_block_table_dev == block_table_dev)) return PIE_ERR_INVALID;
+    if (!words_aligned({block_table_dev, ctx_lens_dev, weights, dst_block_table_dev, weights_out, new_lens_dev, kept_dev})) return PIE_ERR_INVALID;
+    const int64_t pairs = (int64_t)n_seqs * pool->cfg.n_kv_heads;
     if (!weights_out) {
         weights_out = weights;
         weights_out_stride = weights_stride;
     } else if (weights_out_stride <= 0 || (weights_out == weights && weights_out_stride != weights_stride)) {
         return PIE_ERR_INVALID;
+    } else if (weights_out != weights && n_seqs > 0) {   // a row written must not be another that is still to be read
+        const uintptr_t in = (uintptr_t)weights, out = (uintptr_t)weights_out;
+        if (in < out + (uintptr_t)(pairs * weights_out_stride) * 4 && out < in + (uintptr_t)(pairs * weights_stride) * 4) return PIE_ERR_INVALID;
     }
-    const int64_t pairs = (int64_t)n_seqs * pool->cfg.n_kv_heads;
     pie::EvictLaunch a{};
     a.block_table = block_table_dev;
     a.ctx_lens = ctx_lens_dev;
@@ -2330,6 +2343,8 @@ int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, 
     a.n_seqs = n_seqs;
     a.budget = budget;
     a.recent = recent;
+    // (a sequence keeps no more tokens than its table and its weights hold: a larger budget needs no larger scratch)
+    a.rows_stride = (int32_t)std::min<int64_t>(budget, std::min<int64_t>((int64_t)max_blocks_per_seq * 16, weights_stride));
     a.status = pool->status_dev;
     if (pairs * std::max<int64_t>(1, pie::evict_chunks(a)) > 0x7fffffffll) return PIE_ERR_INVALID;
     OnDevice on(pool->device);
@@ -2344,7 +2359,7 @@ int pie_kv_evict(pie_pool *pool, int32_t layer, const int32_t *block_table_dev, 
         pool->evict_ready = true;
     }
     // scratch: the kept tokens' rows and the counts; grows when a call needs more (cudaFree waits for the calls before it)
-    const int64_t words = pairs * ((int64_t)budget + 1);
+    const int64_t words = pairs * ((int64_t)a.rows_stride + 1);
     if (words > pool->evict_words) {
         cudaFree(pool->evict_scratch);
         pool->evict_scratch = nullptr;

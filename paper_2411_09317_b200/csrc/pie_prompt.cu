@@ -13,6 +13,12 @@
 //     that sees S(j + 1) knows O += P V of stage j to be complete.
 //   - Eight softmax warps, four per tile, a thread per row: the 128 scores in registers, maximum (three-input), one packed
 //     multiply-add per pair of elements, exponentials, packed sums, P back into TMEM over the scores.
+//   - Two warps clear NaN and infinities from values that some row of the item may not see: a probability of 0 hides all else.
+// A CTA per SM takes items until none is left and goes from one to the next without a break: the next item's query rows, keys and
+// first scores arrive behind the last stage of the item before it.
+// Bound: a stage of both tiles takes some 3300 cycles (2400 of products, the softmax warps' chain beside them) and, under load,
+// the power limit.  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 657 us, 1250 TFLOP/s (half a second of it: 775 us at
+// 1.6 GHz); 16 ragged prompts of 12112 tokens: 140 us; 32 of 512: 125 us; 45 tokens: 8 us, most of it the host's.
 // Scores and sums in fp32.  P is rounded once to the 16-bit type on its way to the tensor core (a second operand with the
 // rounding remainder, as the chunked kernel has for bf16, costs half as many MMAs again and buys less than the output's own
 // rounding); the row's sum is of the unrounded probabilities.
@@ -65,7 +71,7 @@ struct PrSmem {
     static constexpr int OFF_Q = 0;
     static constexpr int OFF_RING = OFF_Q + Q_BYTES;
     static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], clean[4], free[4], s[2], p[2], done[2], q[2], k0
-    static constexpr int OFF_MISC = OFF_BAR + 22 * 8;         // [0] TMEM base, [1] abort, [4 .. 7] items in which a value was not finite
+    static constexpr int OFF_MISC = OFF_BAR + 22 * 8;         // [0] TMEM base, [1] abort, [4], [5] the first and the last item (+ 1) with a value not finite
     static constexpr int BYTES = OFF_MISC + 32;
 };
 
@@ -112,8 +118,8 @@ __device__ __forceinline__ float2 pr_add2(float2 a, float2 b) {
 }
 
 // 2^x for two values at once, in the arithmetic pipes instead of the special-function unit: 2^f for the |f| <= 1/2 that rounding x
-// leaves, by the polynomial of degree 3 with the least relative error there (7.5e-5, from a Remez iteration: an eighth of bf16's
-// half step and a sixth of fp16's), times 2^round(x), put together from its exponent field.  0 below -126.5, and for -inf: what
+// leaves, by the polynomial of degree 3 with the least relative error there (7.5e-5, from a Remez iteration: a fiftieth of
+// bf16's half step and a sixth of fp16's), times 2^round(x), put together from its exponent field.  0 below -126.5, and for -inf: what
 // is masked is nothing at all.
 __device__ __forceinline__ float2 pr_exp2_poly(float2 x) {
     x.x = fmaxf(x.x, -127.f);
@@ -153,7 +159,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     constexpr int RING = SM::RING;
     // Share of the exponentials, in eighths, that the arithmetic pipes take over from the special-function unit (16 a clock and SM:
     // as long for a stage's exponentials as the tensor core for its products).  More of them costs more instructions than the
-    // unit's relief gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128: 0, 1, 2, 3 eighths 679, 665, 673, 689 us; 16
+    // unit's relief gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128: 0, 1, 2, 3 eighths 679, 665, 673, 689 us (side by side); 16
     // ragged prompts: 176, 161, 161, 176 us.
     constexpr int POLY = 1;
     extern __shared__ __align__(1024) uint8_t pr_smem[];
@@ -165,9 +171,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         return;
     }
     // A CTA works through its items without a break: the stages of all of them form one sequence g = 0, 1, ...  Ring entry 2 g
-    // is K, 2 g + 1 is V of stage g.  full[g & 3]: V(g) and K(g + 1) have landed; clean[g & 3]: and V(g) may be multiplied.  free[f & 3]: f = 0: the first scores, f = g + 1:
-    // all MMAs of stage g (O += P V of both tiles and the next scores) are complete.  Per tile: s: scores complete, p: P in place,
-    // done: O of the item complete, q: its query rows have landed.
+    // is K, 2 g + 1 is V of stage g.  full[g & 3]: V(g) and K(g + 1) have landed; clean[g & 3]: and V(g) may be multiplied.
+    // free[f & 3]: f = 0: the first scores, f = g + 1: all MMAs of stage g (O += P V of both tiles and the next scores) are
+    // complete.  Per tile: s: scores complete, p: P in place, done: O of the item complete, q: its query rows have landed.
     const uint32_t bar_full = base + SM::OFF_BAR, bar_clean = bar_full + 32, bar_free = bar_clean + 32, bar_s = bar_free + 32, bar_p = bar_s + 16, bar_done = bar_p + 16;
     const uint32_t bar_q = bar_done + 16, bar_k0 = bar_q + 16;
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
@@ -199,8 +205,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             pf_mbar_init(bar_full + 8 * i, 1);
             pf_mbar_init(bar_clean + 8 * i, 2);   // warps 10 and 11
             pf_mbar_init(bar_free + 8 * i, 1);
-            misc[4 + i] = 0;
         }
+        misc[4] = 0xffffffffu;
+        misc[5] = 0;
         pf_mbar_init(bar_k0, 1);
         for (int t = 0; t < 2; ++t) {
             pf_mbar_init(bar_q + 8 * t, 1);
@@ -321,7 +328,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // =============================================================================== the issuing warp
         // The operands are warp-uniform values and the branch is an elected lane's, so that the MMAs take them from uniform
         // registers as they come: formed in the branch of lane 0, each MMA waited for the moves (863 us for 10007 tokens), issued
-        // without a branch, by a predicate, it cost some ten instructions (715 us; so 679 us).  TMEM: all 512 columns are this
+        // without a branch, by a predicate, it cost some ten instructions (715 us; so 679 us, the rest of the kernel as it was then).  TMEM: all 512 columns are this
         // CTA's, so its base is column 0.
         constexpr uint32_t IDESC_S = instr_desc(BF16, PR_KV, false), IDESC_O = instr_desc(BF16, D, true);
         const uint64_t q_desc = smem_desc(base + SM::OFF_Q, 16, 1024), k_desc = smem_desc(base + SM::OFF_RING, 16, 1024);
@@ -432,7 +439,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                 }
                     }
                     if (found) {
-                        misc[4 + (k & 3)] = (uint32_t)k + 1u;
+                        atomicMin(const_cast<uint32_t *>(misc + 4), (uint32_t)k + 1u);
+                        atomicMax(const_cast<uint32_t *>(misc + 5), (uint32_t)k + 1u);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                 }
@@ -461,7 +469,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int32_t first = tok0 + t * TT;                          // the tile's first position
         const int32_t my_pos = first + my_tok;
         const bool row_valid = my_tok < TT && my_pos < it.len;
-                float m_run = -INFINITY, l_run = 0.f;
+        float m_run = -INFINITY, l_run = 0.f;
         bool spoiled = false;                                         // a score the row sees is NaN or +inf: so is the softmax
         for (int32_t j = 0; j < n; ++j) {
             if (!wait_all(bar_s + 8 * t, s_count & 1u)) { ok = false; break; }
@@ -542,7 +550,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             tc_fence_after();
             const float inv = spoiled ? __int_as_float(0x7fc00000) : 1.f / l_run;
             const bool wide_out = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;
-            const bool repair = misc[4 + (k & 3)] == (uint32_t)k + 1u;
+            // (items between the first and the last such item look for nothing in vain; a flag per item could be overwritten while a
+            // tile that has no part in the items in between is still behind)
+            const bool repair = misc[4] <= (uint32_t)k + 1u && (uint32_t)k + 1u <= misc[5];
             uint4 *dst = reinterpret_cast<uint4 *>(p.out + ((int64_t)(it.seq0 + my_pos) * p.n_q_heads + it.kvh * G + my_g) * D);
             const uint16_t *vrow = p.v + (int64_t)(it.seq0 + tok0 + 1) * p.v_stride + (int64_t)it.kvh * D;
 #pragma unroll 1

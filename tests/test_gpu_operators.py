@@ -275,7 +275,8 @@ def test_rope_refusals():
         for kw in (dict(q=q + 2), dict(ko=ko + 8), dict(v=None), dict(k=None, ko=None), dict(seq=None), dict(place=None), dict(pos=None),
                    dict(qo=None), dict(q=None), dict(bt=None, ko=None), dict(n=-1), dict(mb=0), dict(s=0), dict(q_stride=255), dict(q_stride=260),
                    dict(k_stride=64), dict(v_stride=120), dict(qo=q + 512), dict(ko=k + 256), dict(qo=k), dict(ko=v), dict(ko=qo),
-                   dict(qo=q, q_stride=512), dict(q=None, qo=None, k=None, ko=None, bt=None)):
+                   dict(qo=q, q_stride=512), dict(q=None, qo=None, k=None, ko=None, bt=None), dict(pos=i + 2), dict(seq=i + 1), dict(place=i + 2),
+                   dict(bt=i + 2), dict(q_stride=1 << 40)):
             refused(pie.PIE_ERR_INVALID, call, **kw)
         refused(pie.PIE_ERR_RANGE, call, layer=1)
         refused(pie.PIE_ERR_RANGE, call, layer=-1)
@@ -384,6 +385,25 @@ def test_prompt_masked_places_cannot_reach_a_row(dtype, d, value):
         o, e = args[3][s], args[3][s + 1]
         assert np.array_equal(got[o:o + t], clean[o:o + t])
         assert value != "nan" or np.all(np.isnan(got[o + t:e]))
+
+
+@pytest.mark.parametrize("value", [0x7fc0, 0xff80])
+def test_prompt_values_not_finite_in_every_item(value):
+    """Many more items than CTAs, of one tile and of two in every order, each with NaN or -inf in the last value of its sequence: a
+    row but the last is as without it, the last one gets the value in its column."""
+    lens = [(1, 130, 20, 3, 257, 32, 9, 64, 65, 2)[i % 10] for i in range(400)]
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+
+    def poison(k, v, off):
+        v[off[1:] - 1, :, 3] = value
+
+    clean, _ = run_prompt(8, 2, 64, BF16, lens, 150)
+    got, _ = run_prompt(8, 2, 64, BF16, lens, 150, poison=poison)
+    last = np.zeros(len(got), bool)
+    last[off[1:] - 1] = True
+    assert np.array_equal(got[~last], clean[~last])
+    assert np.array_equal(np.delete(got[last], 3, axis=2), np.delete(clean[last], 3, axis=2))
+    assert np.all(np.isnan(got[last][:, :, 3]) if value == 0x7fc0 else got[last][:, :, 3] == -np.inf)
 
 
 def test_prompt_repeats_bit_for_bit_and_on_two_pools_at_once():
@@ -621,6 +641,32 @@ def test_evict_optional_outputs_and_aliased_lengths():
     run_evict(4, 2, 64, F16, [60, 130, 0, 7], 50, 20, 331, alias_lens=True, in_place=True)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_with_a_budget_beyond_every_table(in_place):
+    """The largest budget: every sequence keeps everything; out of place that is a copy."""
+    lens = [40, 0, 21]
+    with Pool(4, 2, 64, F16, 10) as p:
+        data = p.random(345)
+        p.fill(data)
+        tab, dst = np.array([[0, 1, 2], [0, 0, 0], [3, 4, 0]], np.int32), np.array([[5, 6, 7], [0, 0, 0], [8, 9, 0]], np.int32)
+        w0 = np.random.default_rng(1).random((3, 2, 48)).astype(np.float32)
+        w, w_out = up(w0), torch.zeros((3, 2, 48), dtype=torch.float32, device=DEV)
+        dt, dd, ctx = up(tab), up(dst), up(np.array(lens, np.int32))
+        new = torch.zeros(3, dtype=torch.int32, device=DEV)
+        pie.pie_kv_evict(p.h, 0, dt.data_ptr(), 3, ctx.data_ptr(), 3, w.data_ptr(), 48, 2 ** 31 - 1, 2 ** 31 - 1 if in_place else 0,
+                         dst_block_table_dev=None if in_place else dd.data_ptr(), dst_max_blocks=0 if in_place else 3,
+                         weights_out=w_out.data_ptr(), weights_out_stride=48, new_lens_dev=new.data_ptr())
+        pie.pie_sync(p.h)
+        assert new.cpu().numpy().tolist() == lens
+        want = data.copy()
+        for s, n in enumerate(lens):
+            assert np.array_equal(w_out[s, :, :n].cpu().numpy(), w0[s, :, :n])
+            if not in_place:
+                t = np.arange(n)
+                want[dst[s, t // 16], :, :, t % 16] = data[tab[s, t // 16], :, :, t % 16]
+        assert np.array_equal(p.raw(), want)
+
+
 def test_evict_leaves_a_sequence_alone_that_is_not_all_there():
     with Pool(4, 2, 64, F16, 12, host_slots=16) as p:
         data = p.random(340)
@@ -667,7 +713,10 @@ def test_evict_refusals():
 
         for kw in (dict(bt=None), dict(mb=0), dict(ctx=None), dict(n=-1), dict(wp=None), dict(stride=0), dict(budget=0), dict(recent=-1),
                    dict(recent=5), dict(dst_block_table_dev=i + 128, dst_max_blocks=0), dict(dst_block_table_dev=i, dst_max_blocks=1),
-                   dict(weights_out=w.data_ptr(), weights_out_stride=16), dict(weights_out=w.data_ptr() + 64, weights_out_stride=0)):
+                   dict(weights_out=w.data_ptr(), weights_out_stride=16), dict(weights_out=w.data_ptr() + 64, weights_out_stride=0),
+                   dict(weights_out=w.data_ptr() + 64, weights_out_stride=16), dict(weights_out=w.data_ptr() - 64, weights_out_stride=16),
+                   dict(bt=i + 2), dict(ctx=i + 66), dict(wp=w.data_ptr() + 2), dict(new_lens_dev=i + 129), dict(kept_dev=i + 130),
+                   dict(dst_block_table_dev=i + 129, dst_max_blocks=1), dict(weights_out=w.data_ptr() + 1026, weights_out_stride=32)):
             refused(pie.PIE_ERR_INVALID, call, **kw)
         refused(pie.PIE_ERR_RANGE, call, layer=1)
         call(n=0)
