@@ -17,8 +17,10 @@
 // A CTA per SM takes items until none is left and goes from one to the next without a break: the next item's query rows, keys and
 // first scores arrive behind the last stage of the item before it.
 // Bound: a stage of both tiles takes some 3300 cycles (2400 of products, the softmax warps' chain beside them) and, under load,
-// the power limit.  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 657 us, 1250 TFLOP/s (half a second of it: 775 us at
-// 1.6 GHz); 16 ragged prompts of 12112 tokens: 140 us; 32 of 512: 125 us; 45 tokens: 8 us, most of it the host's.
+// the power limit.  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 655 us, 1250 TFLOP/s (half a second of it: 775 us at
+// 1.6 GHz); 16 ragged prompts of 12112 tokens: 128 us; 32 of 512: 112 us; 45 tokens: 7 us, most of it the host's.  Short prompts
+// pay 1.4 us per item for the epilogue, whose stores take a line per lane: exchanging sectors between two lanes or four first costs
+// as much as it saves (128 and 130 us for the ragged prompts).
 // Scores and sums in fp32.  P is rounded once to the 16-bit type on its way to the tensor core (a second operand with the
 // rounding remainder, as the chunked kernel has for bf16, costs half as many MMAs again and buys less than the output's own
 // rounding); the row's sum is of the unrounded probabilities.
@@ -49,7 +51,8 @@ constexpr int PR_TMEM_COLS = 512;             // S0, S1 (128 each; P over them),
 // hardly any stage rescales.
 constexpr float PR_LAZY = 8.f;
 
-constexpr int PR_INLINE = 192;   // items that travel with the launch's parameters: no copy in front of a small call
+constexpr int PR_INLINE = 480;   // items that travel with the launch's parameters (7.5 KiB): no copy in front of the call.  It saves 7 us
+                                 // (16 ragged prompts: 135 -> 128 us); with 960 a call of 45 tokens takes 0.5 us longer, with 1900 1.8 us
 
 struct PromptParams {
     const int4 *items;       // {first token of the sequence, first token of the item (within it), sequence length, -}; NULL: inline
@@ -463,9 +466,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         bool more = get_item(0, it), ok = true;
         uint32_t s_count = 0, done_count = 0;
         for (int32_t k = 0; more && ok; ++k, it = next) {
-        more = get_item(k + 1, next);
         const int32_t n = t == 0 ? it.n0 : it.n1, tok0 = it.tok0;
-        if (n == 0) continue;
+        if (n == 0) {
+            more = get_item(k + 1, next);
+            continue;
+        }
         const int32_t first = tok0 + t * TT;                          // the tile's first position
         const int32_t my_pos = first + my_tok;
         const bool row_valid = my_tok < TT && my_pos < it.len;
@@ -483,13 +488,18 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const bool masked = t_base + PR_KV - 1 > first;           // some row of the tile does not see the whole stage
             float scale = p.scale_log2e;
             if (masked || scale <= 0.f) {
-                // scores in log2 units, what a row may not see at -inf (by selection: NaN scores too)
+                if (scale <= 0.f) {                                   // (the maximum is taken of the scaled scores)
 #pragma unroll
-                for (int c = 0; c < 128; ++c) {
-                    const float x = __uint_as_float(sv[c >> 5][c & 31]) * scale;
-                    sv[c >> 5][c & 31] = __float_as_uint(t_base + c <= my_pos ? x : -INFINITY);
+                    for (int c = 0; c < 128; ++c) sv[c >> 5][c & 31] = __float_as_uint(__uint_as_float(sv[c >> 5][c & 31]) * scale);
+                    scale = 1.f;
                 }
-                scale = 1.f;
+                // what a row may not see becomes -inf (by selection: NaN scores too), in the quarters that some row does not see whole
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (t_base + 32 * u + 31 > first) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) sv[u][c] = t_base + 32 * u + c <= my_pos ? sv[u][c] : 0xff800000u;
+                    }
             }
             float a0 = -INFINITY, a1 = -INFINITY, a2 = -INFINITY, a3 = -INFINITY;
 #pragma unroll
@@ -542,6 +552,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             __syncwarp();
             if (lane == 0) pf_mbar_arrive(bar_p + 8 * t);
         }
+        more = get_item(k + 1, next);                                 // (looked up while the last products run)
         if (ok) ok = wait_all(bar_done + 8 * t, done_count & 1u);
         ++done_count;
         // ---- out = O / l, rounded to the 16-bit type (nearest even).  The TMEM loads are warp-wide: rows beyond the tile take
