@@ -8,7 +8,9 @@
 //   - The loading warp brings the Q tiles and the K and V stages (128 tokens; TMA tiles of 64 elements, 128-byte swizzle) through
 //     a ring of stage buffers: K0, V0, K1, V1, ...
 //   - One thread of the issuing warp issues the MMAs.  Per tile and stage: S = Q K^T (128 x 128 x D, fp32, 128 TMEM columns) and
-//     O += P V (D TMEM columns) with P read from TMEM.  The order is O0 += P0 V(j), S0(j + 1), O1 += P1 V(j), S1(j + 1): tcgen05
+//     O += P V (D TMEM columns) with P read from TMEM, in two halves of the stage's tokens, so that the first half's products run
+//     beside the second half's exponentials (642 -> 636 us for 10007 tokens, 127 -> 124 us for the ragged prompts; in quarters, or
+//     three quarters and one: 643 and 647, 125 and 126).  The order is O0 += P0 V(j), S0(j + 1), O1 += P1 V(j), S1(j + 1): tcgen05
 //     MMAs of one thread complete in order, so S may follow O += P V over the same columns without a wait, and a softmax warp
 //     that sees S(j + 1) knows O += P V of stage j to be complete.
 //   - Eight softmax warps, four per tile, a thread per row: the 128 scores in registers, maximum (three-input), one packed
@@ -17,8 +19,8 @@
 // A CTA per SM takes items until none is left and goes from one to the next without a break: the next item's query rows, keys and
 // first scores arrive behind the last stage of the item before it.
 // Bound: a stage of both tiles takes some 3300 cycles (2400 of products, the softmax warps' chain beside them) and, under load,
-// the power limit.  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 655 us, 1250 TFLOP/s (half a second of it: 775 us at
-// 1.6 GHz); 16 ragged prompts of 12112 tokens: 128 us; 32 of 512: 112 us; 45 tokens: 7 us, most of it the host's.  Short prompts
+// the power limit.  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 636 us, 1290 TFLOP/s (half a second of it: 750 us at
+// 1.63 GHz); 16 ragged prompts of 12112 tokens: 124 us; 32 of 512: 108 us; 45 tokens: 7 us, most of it the host's.  Short prompts
 // pay 1.4 us per item for the epilogue, whose stores take a line per lane: exchanging sectors between two lanes or four first costs
 // as much as it saves (128 and 130 us for the ragged prompts).
 // Scores and sums in fp32.  P is rounded once to the 16-bit type on its way to the tensor core (a second operand with the
@@ -73,8 +75,8 @@ struct PrSmem {
     static constexpr int RING = D == 128 ? 5 : 8;
     static constexpr int OFF_Q = 0;
     static constexpr int OFF_RING = OFF_Q + Q_BYTES;
-    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], clean[4], free[4], s[2], p[2], done[2], q[2], k0
-    static constexpr int OFF_MISC = OFF_BAR + 22 * 8;         // [0] TMEM base, [1] abort, [4], [5] the first and the last item (+ 1) with a value not finite
+    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], clean[4], free[4], s[2], pa[2], pb[2], done[2], q[2], k0
+    static constexpr int OFF_MISC = OFF_BAR + 24 * 8;         // [0] TMEM base, [1] abort, [4], [5] the first and the last item (+ 1) with a value not finite
     static constexpr int BYTES = OFF_MISC + 32;
 };
 
@@ -105,13 +107,6 @@ __device__ __forceinline__ float2 pr_fma2(float2 a, float2 b, float2 c) {
         : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
     return r;
 }
-__device__ __forceinline__ float2 pr_mul2(float2 a, float2 b) {
-    float2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;"
-        : "=l"(*reinterpret_cast<uint64_t *>(&r))
-        : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
-    return r;
-}
 __device__ __forceinline__ float2 pr_add2(float2 a, float2 b) {
     float2 r;
     asm("add.rn.f32x2 %0, %1, %2;"
@@ -120,22 +115,16 @@ __device__ __forceinline__ float2 pr_add2(float2 a, float2 b) {
     return r;
 }
 
-// 2^x for two values at once, in the arithmetic pipes instead of the special-function unit: 2^f for the |f| <= 1/2 that rounding x
-// leaves, by the polynomial of degree 3 with the least relative error there (7.5e-5, from a Remez iteration: a fiftieth of
-// bf16's half step and a sixth of fp16's), times 2^round(x), put together from its exponent field.  0 below -126.5, and for -inf: what
-// is masked is nothing at all.
-__device__ __forceinline__ float2 pr_exp2_poly(float2 x) {
-    x.x = fmaxf(x.x, -127.f);
-    x.y = fmaxf(x.y, -127.f);
-    const float2 magic = make_float2(12582912.f, 12582912.f), unmagic = make_float2(-12582912.f, -12582912.f);
-    const float2 t = pr_add2(x, magic);            // the rounded value in the low bits
-    const float2 n = pr_add2(t, unmagic);
-    const float2 f = pr_fma2(n, make_float2(-1.f, -1.f), x);
-    float2 y = pr_fma2(f, make_float2(0.0551716685f, 0.0551716685f), make_float2(0.242611125f, 0.242611125f));
-    y = pr_fma2(y, f, make_float2(0.693260968f, 0.693260968f));
-    y = pr_fma2(y, f, make_float2(0.999928057f, 0.999928057f));
-    const float2 s = make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u));
-    return pr_mul2(y, s);
+__device__ __forceinline__ void pr_tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void pr_tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
 }
 
 // largest magnitude bits of the two halves of each word; >= EXP in a half: that value is not finite
@@ -160,11 +149,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     using SM = PrSmem<D>;
     constexpr int HALVES = D / 64;
     constexpr int RING = SM::RING;
-    // Share of the exponentials, in eighths, that the arithmetic pipes take over from the special-function unit (16 a clock and SM:
-    // as long for a stage's exponentials as the tensor core for its products).  More of them costs more instructions than the
-    // unit's relief gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128: 0, 1, 2, 3 eighths 679, 665, 673, 689 us (side by side); 16
-    // ragged prompts: 176, 161, 161, 176 us.
-    constexpr int POLY = 1;
+    // (All exponentials in the special-function unit, 16 a clock and SM: as long for a stage's as the tensor core for its products.
+    // An eighth, a quarter, three eighths of them by a polynomial in the arithmetic pipes cost as many instructions as that relief
+    // gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128: 0, 1, 2, 3 eighths 649, 653, 654, 685 us; 16 ragged prompts:
+    // 127, 127, 128, 149 us; heads of 64: 585, 594, 564, 619 us.)
     extern __shared__ __align__(1024) uint8_t pr_smem[];
     uint8_t *smem = pr_smem;
     const uint32_t base = pf_smem_u32(pr_smem);
@@ -176,9 +164,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     // A CTA works through its items without a break: the stages of all of them form one sequence g = 0, 1, ...  Ring entry 2 g
     // is K, 2 g + 1 is V of stage g.  full[g & 3]: V(g) and K(g + 1) have landed; clean[g & 3]: and V(g) may be multiplied.
     // free[f & 3]: f = 0: the first scores, f = g + 1: all MMAs of stage g (O += P V of both tiles and the next scores) are
-    // complete.  Per tile: s: scores complete, p: P in place, done: O of the item complete, q: its query rows have landed.
-    const uint32_t bar_full = base + SM::OFF_BAR, bar_clean = bar_full + 32, bar_free = bar_clean + 32, bar_s = bar_free + 32, bar_p = bar_s + 16, bar_done = bar_p + 16;
-    const uint32_t bar_q = bar_done + 16, bar_k0 = bar_q + 16;
+    // complete.      // complete.  Per tile: s: scores complete, pa, pb: the halves of P in place, done: O of the item complete, q: its query rows
+    // have landed.
+    const uint32_t bar_full = base + SM::OFF_BAR, bar_clean = bar_full + 32, bar_free = bar_clean + 32, bar_s = bar_free + 32, bar_pa = bar_s + 16, bar_pb = bar_pa + 16;
+    const uint32_t bar_done = bar_pb + 16, bar_q = bar_done + 16, bar_k0 = bar_q + 16;
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
 
     // ---- the CTA's items: the list goes from long to short, and every other pass over the CTAs runs backwards, so that all get
@@ -215,7 +204,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         for (int t = 0; t < 2; ++t) {
             pf_mbar_init(bar_q + 8 * t, 1);
             pf_mbar_init(bar_s + 8 * t, 1);
-            pf_mbar_init(bar_p + 8 * t, 4);   // a warp each
+            pf_mbar_init(bar_pa + 8 * t, 4);   // a warp each
+            pf_mbar_init(bar_pb + 8 * t, 4);
             pf_mbar_init(bar_done + 8 * t, 1);
         }
         misc[1] = 0;
@@ -349,6 +339,19 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             __syncwarp();
         };
+        // O += P V of half the stage's tokens
+        auto issue_o = [&](int t, int half, uint64_t vd, bool add, bool last = false) {
+            tc_fence_after();
+            if (pr_elect()) {
+#pragma unroll
+                for (int i = 0; i < PR_KV / 32; ++i) {   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
+                    const int ks = half * (PR_KV / 32) + i;
+                    mma_f16_ts(256 + t * 128, t * 128 + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), IDESC_O, (add || i > 0) ? 1u : 0u);
+                }
+                if (last) tc_commit(bar_done + 8 * t);
+            }
+            __syncwarp();
+        };
         Item it, next;
         bool more = get_item(0, it), ok = true;
         uint32_t p_count[2] = {0, 0}, q_count[2] = {0, 0};
@@ -378,17 +381,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (int t = 0; t < 2; ++t) {
                     const int32_t n = t == 0 ? it.n0 : it.n1, nx = t == 0 ? nx0 : nx1;
                     if (ok && j < n) {
-                        ok = wait_all(bar_p + 8 * t, p_count[t] & 1u);
+                        // (the first half's products run while the softmax warps work on the second)
+                        ok = wait_all(bar_pa + 8 * t, p_count[t] & 1u);
+                        if (ok) {
+                            issue_o(t, 0, vd, j > 0);
+                            ok = wait_all(bar_pb + 8 * t, p_count[t] & 1u);
+                        }
                         ++p_count[t];
                         if (!ok) continue;
-                        tc_fence_after();
-                        if (pr_elect()) {
-#pragma unroll
-                            for (int ks = 0; ks < PR_KV / 16; ++ks)   // V: 16 tokens further per step, 64-element chunks of D are 16 KiB apart
-                                mma_f16_ts(256 + t * 128, t * 128 + ks * 8, vd + (uint64_t)(ks * 2048 >> 4), IDESC_O, (j > 0 || ks > 0) ? 1u : 0u);
-                            if (j + 1 == n) tc_commit(bar_done + 8 * t);
-                        }
-                        __syncwarp();
+                        issue_o(t, 1, vd, true, j + 1 == n);
                     }
                     if (ok && (j + 1 < n || (last && nx > 0))) {   // the item's next scores, or the next item's first
                         if (j + 1 >= n) {
@@ -517,6 +518,19 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const float alpha = grow ? pf_exp2(m_run - m_cand) : 1.f; // (m_run = -inf gives 0: nothing accumulated yet)
             m_run = m_new;
             const float neg_m = m_new == -INFINITY ? 0.f : -m_new;    // (a row that has seen nothing: exponents stay -inf)
+            // ---- O *= alpha where a row's maximum moved (skipped by warps in which none did; few columns at a time: the scores
+            // are in registers)
+            if (j >= 1 && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 8) {
+                    uint32_t ov[8];
+                    pr_tmem_ld8(tmem_o + c0, ov);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * alpha);
+                    pr_tmem_st8(tmem_o + c0, ov);
+                }
+            }
             const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(neg_m, neg_m);
             float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
@@ -526,31 +540,25 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (int w = 0; w < 32; ++w) {
                     const int c = 64 * h + 2 * w;
                     const float2 x = pr_fma2(make_float2(__uint_as_float(sv[c >> 5][c & 31]), __uint_as_float(sv[c >> 5][(c & 31) + 1])), sc2, nm2);
-                    const float2 e = (w & 7) < POLY ? pr_exp2_poly(x) : make_float2(pf_exp2(x.x), pf_exp2(x.y));
+                    const float2 e = make_float2(pf_exp2(x.x), pf_exp2(x.y));
                     if (w & 1) s1 = pr_add2(s1, e);
                     else s0 = pr_add2(s0, e);
                     pw[w] = pf_pack2<BF16>(e.x, e.y);
+                    if (h == 1 && w == 7) {                           // the first half is in place (stored long enough ago not to wait)
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) pf_mbar_arrive(bar_pa + 8 * t);
+                    }
                 }
                 tmem_st32(tmem_s + 32 * h, pw);   // a thread overwrites only its own row's scores, which it has read
             }
             s0 = pr_add2(s0, s1);
             l_run = l_run * alpha + (s0.x + s0.y);
-            // ---- O *= alpha where a row's maximum moved (skipped by warps in which none did)
-            if (j >= 1 && __any_sync(0xffffffffu, alpha != 1.f)) {
-#pragma unroll
-                for (int c0 = 0; c0 < D; c0 += 32) {
-                    uint32_t ov[32];
-                    tmem_ld32(tmem_o + c0, ov);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * alpha);
-                    tmem_st32(tmem_o + c0, ov);
-                }
-            }
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) pf_mbar_arrive(bar_p + 8 * t);
+            if (lane == 0) pf_mbar_arrive(bar_pb + 8 * t);
         }
         more = get_item(k + 1, next);                                 // (looked up while the last products run)
         if (ok) ok = wait_all(bar_done + 8 * t, done_count & 1u);
