@@ -11,6 +11,8 @@
 // halves of eight pairs in either pair layout) of one token, with the pairs' factors in registers, and walks over heads: two
 // 16-byte loads and two 16-byte stores per destination each, the next heads' loads in flight.  The query heads come first: the
 // chain of look-ups that ends in the token's cache row (sequence, block, slot: three dependent loads) hides behind them.
+// Bound: bytes.  16411 tokens of 64 + 8 + 8 heads of 128 (706 MB) in 135 us, 5.2 TB/s, 81 % of a plain copy's rate; 2045 tokens of
+// 32 + 8 + 8 into an 8-bit cache (50 MB) in 15.5 us, half the floor's speed: launch, the wait for the positions and one wave's tail.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -237,8 +239,7 @@ rope_kv_kernel(const __grid_constant__ RopeParams p) {
 }
 
 template <typename F>
-cudaError_t dispatch_rope(const AttnShape &sh, bool few, F &&f) {
-    // few tokens: one per CTA
+cudaError_t dispatch_rope(const AttnShape &sh, bool one, F &&f) {   // one token per CTA, or four
     auto by_type = [&](auto d, auto t) -> cudaError_t {
         constexpr int D = decltype(d)::value, T = decltype(t)::value;
         if (sh.kv_fp8) return sh.dtype == PIE_BF16 ? f(rope_kv_kernel<128, T, true, true>, T) : f(rope_kv_kernel<128, T, false, true>, T);
@@ -248,15 +249,15 @@ cudaError_t dispatch_rope(const AttnShape &sh, bool few, F &&f) {
     using C128 = std::integral_constant<int, 128>;
     using One = std::integral_constant<int, 1>;
     using Four = std::integral_constant<int, 4>;
-    if (sh.head_dim == 128) return few ? by_type(C128(), One()) : by_type(C128(), Four());
-    return few ? by_type(C64(), One()) : by_type(C64(), Four());
+    if (sh.head_dim == 128) return one ? by_type(C128(), One()) : by_type(C128(), Four());
+    return one ? by_type(C64(), One()) : by_type(C64(), Four());
 }
 
 }  // namespace
 
 cudaError_t rope_configure(const AttnShape &sh) {
-    for (const bool few : {true, false}) {
-        const cudaError_t e = dispatch_rope(sh, few, [](auto kernel, int) {
+    for (const bool one : {true, false}) {
+        const cudaError_t e = dispatch_rope(sh, one, [](auto kernel, int) {
             return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         });
         if (e != cudaSuccess) return e;
@@ -299,8 +300,12 @@ cudaError_t launch_rope_kv(const AttnShape &sh, const RopeLaunch &a, const RopeT
     };
     p.k_inv = exact_inverse(a.k_scale);
     p.v_inv = exact_inverse(a.v_scale);
-    // Four tokens per CTA once that still gives every SM several CTAs; below, one: a decode step's latency is what counts there
-    return dispatch_rope(sh, a.n_tokens < 4 * n_sms, [&](auto kernel, int tokens) {
+    // Tokens per CTA: four where a token has few rows per thread (one token per CTA, four: 32 + 8 + 8 heads of 128, 16411 tokens 98
+    // and 86 us; 8 + 2 + 2: 77 and 35; 32 + 8 + 8 of 64: 68 and 47), one where a thread has two and a half of them anyway (64 + 8 + 8:
+    // 134 and 137 us; 32 + 32 + 32: 170 and 182) and where four would leave SMs without a CTA (500 tokens, 32 + 32 + 32: 8.3 and 12.4
+    // us; 64 + 8 + 8: 6.5 and 9.8).
+    const bool one = a.n_tokens < 4 * n_sms || (sh.n_q_heads + 2 * sh.n_kv_heads) * sh.head_dim >= 40 * ROPE_THREADS;
+    return dispatch_rope(sh, one, [&](auto kernel, int tokens) {
         const int64_t grid = (a.n_tokens + tokens - 1) / tokens;
         if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
         kernel<<<(unsigned)grid, ROPE_THREADS, 0, stream>>>(p);
