@@ -850,3 +850,68 @@ def test_serve_prompts_decode_evict_and_go_on(dtype, fp8):
         for s in range(S):
             assert np.all(np.abs(got_w[s] - added[s]) <= 1.3e-4 * added[s] + 2.0 ** -20 * added[s] + 1e-30)
         p.blocks = p_blocks
+
+
+# ============================================================================================= offsets that pass 32 bits
+def test_far_end_of_a_large_pool():
+    """A pool of 4.6 GB: rotary write, weights and eviction in blocks whose elements' offsets do not fit 32 bits."""
+    hq, hkv, d, blocks = 8, 8, 128, 70000
+    with Pool(hq, hkv, d, F16, blocks, seqs=2) as p:
+        lens = [100, 37]
+        ids = [blocks - 1 - i for i in range(20)]
+        table = np.array([ids[:8], ids[8:16]], np.int32)
+        seq, place = np.repeat([0, 1], lens).astype(np.int32), np.concatenate([np.arange(n) for n in lens]).astype(np.int32)
+        n = sum(lens)
+        k, v, q = rows(400, n, hkv, d, F16), rows(401, n, hkv, d, F16), rows(402, 2, hq, d, F16)
+        freq = frequencies(d)
+        pie.pie_set_rope(p.h, d, [0] * (d // 2), freq)
+        dk, dv, dq, dpos, dseq, dplace, dtab = up(k), up(v), up(q), up(place), up(seq), up(place), up(table)
+        pie.pie_rope_kv_write(p.h, 0, None, None, dk.data_ptr(), None, dv.data_ptr(), dpos.data_ptr(), dseq.data_ptr(), dplace.data_ptr(), n,
+                              dtab.data_ptr(), 8, 2)
+        out, w, ctx = torch.zeros_like(dq), torch.zeros((2, hkv, 128), dtype=torch.float32, device=DEV), up(np.array(lens, np.int32))
+        pie.pie_decode_attention_weights(p.h, 0, dq.data_ptr(), out.data_ptr(), dtab.data_ptr(), 8, ctx.data_ptr(), 2, d ** -0.5, w.data_ptr(), 128)
+        kept = torch.zeros((2, hkv, 40), dtype=torch.int32, device=DEV)
+        pie.pie_sync(p.h)
+        raw = lambda b: pie.pie_block_read(p.h, 0, int(b)).view(np.uint16).reshape(hkv, 2, 16, d)  # noqa: E731
+        before = {b: raw(b) for b in ids}
+        kr, size = oo.rotate(real(k, F16), place[None], np.zeros(d // 2, np.int64), freq, False, 1.0)
+        got_w, off = w.cpu().numpy(), [0, 100, 137]
+        for s, c in enumerate(lens):
+            at = np.arange(c)
+            got_k = np.stack([before[table[s, t // 16]][:, 0, t % 16] for t in at])
+            assert np.all(np.abs(real(got_k, F16) - kr[off[s]:off[s + 1]]) <= U[F16] * np.abs(kr[off[s]:off[s + 1]]) + 1e-6 * size[off[s]:off[s + 1]] + TINY[F16])
+            assert np.array_equal(np.stack([before[table[s, t // 16]][:, 1, t % 16] for t in at]), v[off[s]:off[s + 1]])
+            want = oo.attention_weights(real(q[s], F16), real(got_k, F16), d ** -0.5)
+            assert np.all(np.abs(got_w[s, :, :c] - want) <= 1.3e-4 * want + 1e-30)
+        pie.pie_kv_evict(p.h, 0, dtab.data_ptr(), 8, ctx.data_ptr(), 2, w.data_ptr(), 128, 40, 5, kept_dev=kept.data_ptr())
+        pie.pie_sync(p.h)
+        for h in range(hkv):
+            chosen = oo.keep(got_w[0, h], 100, 40, 5)
+            assert kept[0, h].tolist() == chosen
+            for j, t in enumerate(chosen):
+                assert np.array_equal(raw(table[0, j // 16])[h, :, j % 16], before[table[0, t // 16]][h, :, t % 16])
+
+
+def test_prompt_rows_beyond_32_bits():
+    """Query and output arrays of more than 2^32 bytes and 2^31 elements: the last sequences against the same ones alone."""
+    hq, hkv, d = 64, 8, 128
+    lens = [128] * 2080
+    n = sum(lens)
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    assert n * hq * d > 1 << 31
+    g = torch.Generator(device=DEV).manual_seed(7)
+    q, k, v = (torch.randn((n, h, d), generator=g, device=DEV, dtype=torch.bfloat16) for h in (hq, hkv, hkv))
+    out = torch.empty_like(q)
+    with Pool(hq, hkv, d, BF16, 1) as p:
+        torch.cuda.synchronize()
+        pie.pie_prompt_attention(p.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), off, len(lens), d ** -0.5)
+        pie.pie_sync(p.h)
+        part = slice(n - 3 * 128, n)
+        q2, k2, v2 = (x[part].clone() for x in (q, k, v))
+        alone = torch.empty_like(q2)
+        torch.cuda.synchronize()
+        pie.pie_prompt_attention(p.h, q2.data_ptr(), k2.data_ptr(), v2.data_ptr(), alone.data_ptr(), np.array([0, 128, 256, 384], np.int32), 3, d ** -0.5)
+        pie.pie_sync(p.h)
+    assert torch.equal(out[part], alone)
+    bits = lambda x: real(x.view(torch.int16).cpu().numpy(), BF16)  # noqa: E731
+    check_prompt(BF16, bits(alone[:128]), *oo.prompt_attention(bits(q2[:128]), bits(k2[:128]), bits(v2[:128]), np.array([0, 128], np.int32), d ** -0.5))
