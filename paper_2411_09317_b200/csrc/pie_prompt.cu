@@ -18,8 +18,9 @@
 //   - Two warps clear NaN and infinities from values that some row of the item may not see: a probability of 0 hides all else.
 // A CTA per SM takes items until none is left and goes from one to the next without a break: the next item's query rows, keys and
 // first scores arrive behind the last stage of the item before it.
-// Bound: a stage of both tiles takes some 3300 cycles (2400 of products, the softmax warps' chain beside them) and, under load,
-// the power limit.  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 636 us, 1290 TFLOP/s (half a second of it: 750 us at
+// Bound: a stage of both tiles takes some 3300 cycles (2048 of products, as many of exponentials; a tile's chain from scores to
+// scores is longer than the other tile covers) and, under load, the power limit.  Two score buffers of 64 columns per tile, which
+// cut the chain, lose more: a product of 64 columns takes as long as one of 128 (782 us against 638).  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 636 us, 1290 TFLOP/s (half a second of it: 750 us at
 // 1.63 GHz); 16 ragged prompts of 12112 tokens: 124 us; 32 of 512: 108 us; 45 tokens: 7 us, most of it the host's.  Short prompts
 // pay 1.4 us per item for the epilogue, whose stores take a line per lane: exchanging sectors between two lanes or four first costs
 // as much as it saves (128 and 130 us for the ragged prompts).
