@@ -20,10 +20,11 @@
 // first scores arrive behind the last stage of the item before it.
 // Bound: a stage of both tiles takes some 3300 cycles (2048 of products, as many of exponentials; a tile's chain from scores to
 // scores is longer than the other tile covers) and, under load, the power limit.  Two score buffers of 64 columns per tile, which
-// cut the chain, lose more: a product of 64 columns takes as long as one of 128 (782 us against 638).  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 636 us, 1290 TFLOP/s (half a second of it: 750 us at
-// 1.63 GHz); 16 ragged prompts of 12112 tokens: 124 us; 32 of 512: 108 us; 45 tokens: 7 us, most of it the host's.  Short prompts
-// pay 1.4 us per item for the epilogue, whose stores take a line per lane: exchanging sectors between two lanes or four first costs
-// as much as it saves (128 and 130 us for the ragged prompts).
+// cut the chain, lose more: a product of 64 columns takes as long as one of 128 (782 us against 638).  One prompt of 10007 tokens,
+// 32 / 8 heads of 128, bf16: 636 us, 1290 TFLOP/s (half a second of it: 750 us at 1.63 GHz); 16 ragged prompts of 12112 tokens:
+// 124 us; 32 of 512: 108 us; 45 tokens: 7 us, most of it the host's.  Short prompts pay 1.4 us per item for the epilogue, whose
+// stores take a line per lane: exchanging sectors between two lanes or four first costs as much as it saves (128 and 130 us for the
+// ragged prompts, then at 129).
 // Scores and sums in fp32.  P is rounded once to the 16-bit type on its way to the tensor core (a second operand with the
 // rounding remainder, as the chunked kernel has for bf16, costs half as many MMAs again and buys less than the output's own
 // rounding); the row's sum is of the unrounded probabilities.
