@@ -402,7 +402,7 @@ int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out,
  * rounded to nearest.
  * offsets_host: host, n_seqs + 1 entries, first 0, ascending; read before the call returns.  PIE_ERR_INVALID: offsets that are
  * not, pointers or strides not on a 16-byte boundary, a stride below its row, out overlapping an input, more than 131072 pieces
- * of 256 / (n_q_heads / n_kv_heads) tokens (counted per sequence) in one call of a small pool.  PIE_ERR_UNSUPPORTED while the
+ * of 256 / (n_q_heads / n_kv_heads) tokens (an even number, counted per sequence) in one call of a small pool.  PIE_ERR_UNSUPPORTED while the
  * compute stream is being captured. */
 int pie_prompt_attention(pie_pool *pool, const void *q, const void *k, const void *v, void *out, const int32_t *offsets_host,
                          int32_t n_seqs, float scale, int64_t q_stride, int64_t k_stride, int64_t v_stride);
