@@ -225,12 +225,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     }
 
     auto dead = [&]() { return __any_sync(0xffffffffu, misc[1] != 0); };
-    // by every lane of a warp; false: give up (the wait ran out, here or in another warp).  Bounded: about a second.
+    // by every lane of a warp; false: give up (the wait ran out, here or in another warp).  Bounded: about a second.  Lanes may get
+    // different answers from a barrier whose phase completes at that moment, so whether the warp polls on is one vote of all its
+    // lanes: every way out leads through the same votes.
     auto wait_all = [&](uint32_t bar, uint32_t parity) {
-        if (pf_mbar_try_wait(bar, parity)) {
-            __syncwarp();
-            return true;
-        }
+        if (__all_sync(0xffffffffu, pf_mbar_try_wait(bar, parity)) != 0) return true;
         bool there = false;
         for (uint32_t i = 0; i < (1u << 22) && !there; ++i) {
             there = pf_mbar_try_wait(bar, parity);
