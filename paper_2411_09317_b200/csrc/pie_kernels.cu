@@ -645,9 +645,10 @@ cudaError_t launch_kv_write8(const void *k, const void *v, const int32_t *token_
 // One 16-byte piece (four consecutive d of head g) of a sequence's output from its chunk partials: log-sum-exp merge in
 // chunk order, normalised, rounded to the 16-bit type.  get_ml(c) -> {m, l} of chunk c for this head.  Used by the combine
 // kernel and by the deferred combine in the attention kernel's tail: the same arithmetic in the same order, so the same
-// bits whoever merges.
+// bits whoever merges.  (The partials are another grid's writes, read behind the dependency wait: plain pointers and plain loads here and
+// in the callers, for what is promised to be constant as long as the kernel lives may be read ahead of the wait.)
 template <int D, bool BF16, typename GetML>
-__device__ __forceinline__ uint2 merge_piece(const float *__restrict__ part_o, int32_t chunk0, int32_t nchunks, int32_t n_kv_heads,
+__device__ __forceinline__ uint2 merge_piece(const float *part_o, int32_t chunk0, int32_t nchunks, int32_t n_kv_heads,
                                              int32_t kvh, int32_t group, int g, int d, GetML get_ml) {
     float mm = -INFINITY;
     for (int32_t c = 0; c < nchunks; ++c) mm = fmaxf(mm, get_ml(c).x);
@@ -1353,8 +1354,8 @@ constexpr int COMB_CAP = 256;  // chunks per sequence handled through shared mem
 
 // One unit of the merge: slice `slice` of `slices` of head_dim of pair (s, kvh), by NT threads.
 template <int D, bool BF16, int NT>
-__device__ __forceinline__ void combine_unit(float *comb_smem, int tid, int32_t s, int32_t kvh, int slice, int slices, const float *__restrict__ part_o,
-                                             const float *__restrict__ part_ml, const int32_t *__restrict__ chunk_off, uint16_t *__restrict__ out,
+__device__ __forceinline__ void combine_unit(float *comb_smem, int tid, int32_t s, int32_t kvh, int slice, int slices, const float *part_o,
+                                             const float *part_ml, const int32_t *chunk_off, uint16_t *out,
                                              int32_t n_q_heads, int32_t n_kv_heads, int32_t group, int32_t cap) {
     float *wbuf = comb_smem, *lbuf = comb_smem + group * cap;
     const int32_t chunk0 = chunk_off[s], nchunks = chunk_off[s + 1] - chunk0;
@@ -1366,8 +1367,9 @@ __device__ __forceinline__ void combine_unit(float *comb_smem, int tid, int32_t 
         for (int idx = tid; idx < group * nchunks; idx += NT) {
             const int g = idx / nchunks, c = idx - g * nchunks;
             const int64_t id = ((int64_t)(chunk0 + c) * n_kv_heads + kvh) * group + g;
-            wbuf[g * cap + c] = part_ml[id * 2];
-            lbuf[g * cap + c] = part_ml[id * 2 + 1];
+            const float2 x = *reinterpret_cast<const float2 *>(part_ml + id * 2);
+            wbuf[g * cap + c] = x.x;
+            lbuf[g * cap + c] = x.y;
         }
         __syncthreads();
         // every thread works the weights of its head out for itself (a few exponentials, in chunk order: the same
@@ -1401,8 +1403,8 @@ __device__ __forceinline__ void combine_unit(float *comb_smem, int tid, int32_t 
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(COMB_THREADS)
-combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, const int32_t *__restrict__ chunk_off,
-               uint16_t *__restrict__ out, int32_t n_q_heads, int32_t n_kv_heads, int32_t group, int32_t cap) {
+combine_kernel(const float *part_o, const float *part_ml, const int32_t *chunk_off, uint16_t *out,
+               int32_t n_q_heads, int32_t n_kv_heads, int32_t group, int32_t cap) {
     extern __shared__ __align__(16) float comb_smem[];   // wbuf[group][cap], lbuf[group][cap]
     // Launched with programmatic stream serialization: CTAs may become resident while the attention kernel still runs
     // (which hides the launch); nothing that kernel wrote is read before the wait, which returns once the attention
@@ -1431,9 +1433,8 @@ constexpr int FIN_HELD = 16;   // scores that a lane holds
 
 template <int D, bool BF16, int G>
 __global__ void __launch_bounds__(FIN_THREADS)
-attn_finish_kernel(const float *__restrict__ scores, const float *__restrict__ part_o, const float *__restrict__ part_ml,
-                   const int32_t *__restrict__ chunk_off, const int32_t *__restrict__ ctx_lens, uint16_t *__restrict__ out,
-                   float *__restrict__ weights, int64_t stride, int32_t n_seqs, int32_t n_kv_heads, int32_t split_tokens, int32_t max_tokens,
+attn_finish_kernel(const float *scores, const float *part_o, const float *part_ml, const int32_t *chunk_off, const int32_t *ctx_lens,
+                   uint16_t *out, float *weights, int64_t stride, int32_t n_seqs, int32_t n_kv_heads, int32_t split_tokens, int32_t max_tokens,
                    int32_t cap, int32_t slices, int32_t merge_ctas, int32_t *status) {
     extern __shared__ __align__(16) float comb_smem[];
     constexpr int AHEAD = G >= FIN_HELD ? 1 : FIN_HELD / G;   // tokens of a lane at a time
@@ -1474,7 +1475,7 @@ attn_finish_kernel(const float *__restrict__ scores, const float *__restrict__ p
         // the item's sequence: the largest s with chunk_off[s] <= ci
         int32_t seen = 0;
         for (int32_t b = 0; b < n_seqs; b += 32)
-            seen += __popc(__ballot_sync(0xffffffffu, b + lane < n_seqs && __ldg(chunk_off + b + lane) <= ci));
+            seen += __popc(__ballot_sync(0xffffffffu, b + lane < n_seqs && chunk_off[b + lane] <= ci));
         const int32_t s = seen - 1;
         const int32_t chunk0 = chunk_off[s], nchunks = chunk_off[s + 1] - chunk0;
         const int32_t ctx = min(__ldg(ctx_lens + s), max_tokens);
