@@ -77,7 +77,7 @@ struct PrSmem {
     static constexpr int RING = D == 128 ? 5 : 8;
     static constexpr int OFF_Q = 0;
     static constexpr int OFF_RING = OFF_Q + Q_BYTES;
-    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], clean[4], free[4], s[2], pa[2], pb[2], done[2], q[2], k0
+    static constexpr int OFF_BAR = OFF_RING + RING * STAGE;   // full[4], clean[4], free[4], s[2], pa[2], pb[2], done[2], q[2], k0, end
     static constexpr int OFF_MISC = OFF_BAR + 24 * 8;         // [0] TMEM base, [1] abort, [4], [5] the first and the last item (+ 1) with a value not finite
     static constexpr int BYTES = OFF_MISC + 32;
 };
@@ -166,10 +166,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     // A CTA works through its items without a break: the stages of all of them form one sequence g = 0, 1, ...  Ring entry 2 g
     // is K, 2 g + 1 is V of stage g.  full[g & 3]: V(g) and K(g + 1) have landed; clean[g & 3]: and V(g) may be multiplied.
     // free[f & 3]: f = 0: the first scores, f = g + 1: all MMAs of stage g (O += P V of both tiles and the next scores) are
-    // complete.      // complete.  Per tile: s: scores complete, pa, pb: the halves of P in place, done: O of the item complete, q: its query rows
-    // have landed.
+    // complete.  Per tile: s: scores complete, pa, pb: the halves of P in place, done: O of the item complete, q: its query rows
+    // have landed.  k0: the first keys.  end: where the CTA gives up, the MMAs issued by then are complete.
     const uint32_t bar_full = base + SM::OFF_BAR, bar_clean = bar_full + 32, bar_free = bar_clean + 32, bar_s = bar_free + 32, bar_pa = bar_s + 16, bar_pb = bar_pa + 16;
-    const uint32_t bar_done = bar_pb + 16, bar_q = bar_done + 16, bar_k0 = bar_q + 16;
+    const uint32_t bar_done = bar_pb + 16, bar_q = bar_done + 16, bar_k0 = bar_q + 16, bar_end = bar_k0 + 8;
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
 
     // ---- the CTA's items: the list goes from long to short, and every other pass over the CTAs runs backwards, so that all get
@@ -203,6 +203,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         misc[4] = 0xffffffffu;
         misc[5] = 0;
         pf_mbar_init(bar_k0, 1);
+        pf_mbar_init(bar_end, 1);
         for (int t = 0; t < 2; ++t) {
             pf_mbar_init(bar_q + 8 * t, 1);
             pf_mbar_init(bar_s + 8 * t, 1);
@@ -405,6 +406,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 v_slot = k_slot + 1 == RING ? 0 : k_slot + 1;
             }
             it = next;
+        }
+        if (!ok || dead()) {   // giving up: the MMAs in flight still read this CTA's shared memory and write its tensor memory - wait (bounded) for them
+            if (pr_elect()) tc_commit(bar_end);
+            __syncwarp();
+            pf_mbar_wait(bar_end, 0);
         }
         __syncwarp();
     } else {
