@@ -423,8 +423,12 @@ int pie_prompt_plan(const int32_t *offsets, int32_t n_seqs, int32_t item_tokens,
  * clears the entry of a new token, or starts from zeros).  The sums are formed in one fixed order: the same bits every time,
  * wherever the blocks lie.  out and the append are pie_decode_attention's (block_table_host .. v_new may be NULL); where the
  * library chooses the split-K chunk it may take a shorter one here, and out may then differ in its last bits.  A
- * context longer than weights_stride: PIE_ERR_INVALID with host lengths; without them the entries beyond are dropped and the
- * next call returns PIE_ERR_INVALID.  PIE_ERR_UNSUPPORTED while the compute stream is being captured.  The first call on a
+ * context longer than weights_stride: PIE_ERR_INVALID with host lengths; without them the entries beyond are dropped, the others
+ * added, and the next call returns PIE_ERR_INVALID.  A call whose kernel meets a block that is not on the GPU, a context longer than its row of
+ * the table, or a wait that runs out - the next call that checks the device status word returns PIE_ERR_NOT_RESIDENT /
+ * PIE_ERR_INVALID / PIE_ERR_TIMEOUT - adds nothing to any sequence's weights, and may be made again.  Fetches nothing by itself:
+ * the swap-managed calls (pie_decode_step, pie_decode_layer) have no weights, the caller swaps in first.
+ * PIE_ERR_UNSUPPORTED while the compute stream is being captured.  The first call on a
  * pool allocates its scratch (about 4 * n_q_heads bytes per token of the pool, some 20 MiB at least). */
 int pie_decode_attention_weights(pie_pool *pool, int32_t layer, const void *q, void *out, const int32_t *block_table_dev,
                                  int32_t max_blocks_per_seq, const int32_t *ctx_lens_dev, const int32_t *block_table_host,

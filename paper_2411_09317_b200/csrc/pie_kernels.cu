@@ -249,7 +249,7 @@ __device__ __forceinline__ float fast_exp2(float x) {
 // =====================================================================================================
 __global__ void __launch_bounds__(1024)
 plan_kernel(const int32_t *__restrict__ ctx_lens, int32_t n_seqs, int32_t max_tokens, int32_t split_tokens,
-            int32_t max_chunks, int32_t *__restrict__ chunk_off, int32_t *status) {
+            int32_t max_chunks, int32_t *__restrict__ chunk_off, int32_t *status, int32_t *failed, int32_t call) {
     __shared__ int32_t warp_sums[32];
     __shared__ int32_t carry;
     if (threadIdx.x == 0) carry = 0;
@@ -263,6 +263,7 @@ plan_kernel(const int32_t *__restrict__ ctx_lens, int32_t n_seqs, int32_t max_to
             if (ctx > max_tokens) {
                 ctx = max_tokens;
                 raise_status(status, STATUS_CTX_TOO_LONG);
+                if (failed != nullptr) *failed = call;
             }
             v = ctx > 0 ? (ctx + split_tokens - 1) / split_tokens : 0;
         }
@@ -441,6 +442,7 @@ cudaError_t launch_swap_bulk(const void *src_pool, void *dst_pool, const int32_t
 // All waits are bounded: a wait that runs out raises a status word and the CTA leaves through its barriers.
 // =====================================================================================================
 constexpr int ATT_QD = 2;           // depth of the producer -> consumer item queue (item id + its query rows)
+constexpr int ATT_FAILED = 32;      // the counters' word that holds the number of the last weights call that raised a status
 constexpr int ATT_SMEM_SEQS = 1024; // largest batch whose chunk offsets are built in shared memory
 
 struct AttnParams {
@@ -488,6 +490,10 @@ struct AttnParams {
     // Calls that accumulate attention weights (instantiations with SCORES): every valid token's scores, in log2 units, as
     // [item][token of the chunk][head of the group] - see attn_finish_kernel.
     float *scores = nullptr;
+    // ... and the call's number, stored in *failed where the call raises a status: its scores are then those of other blocks or of an
+    // earlier call, and no weight is added.
+    int32_t *failed = nullptr;
+    int32_t call = 0;
 };
 
 // KV8: the pool holds E4M3 bytes; a ring stage is then the 4 KiB byte tile as the TMA unit delivers it, and the consumer
@@ -709,6 +715,10 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
     volatile int32_t *abort_flag = misc;      // [0]
     volatile int32_t *q_item = misc + 4;      // [4 .. 4 + QD)
     int32_t *co_smem = reinterpret_cast<int32_t *>(smem + SM::OFF_CO);
+    auto fail = [&](int32_t flag) {
+        raise_status(p.status, flag);
+        if constexpr (SCORES) *reinterpret_cast<volatile int32_t *>(p.failed) = p.call;
+    };
 
     // Everything up to the dependency wait below touches only shared memory and the call's own inputs (lengths and
     // tables, which no kernel of the path writes): under a programmatic dependent launch it overlaps the tail of the
@@ -741,7 +751,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             int32_t ctx = __ldg(p.ctx_lens + s);
             if (ctx > p.max_blocks * 16) {
                 ctx = p.max_blocks * 16;
-                if (blockIdx.x == 0) raise_status(p.status, STATUS_CTX_TOO_LONG);
+                if (blockIdx.x == 0) fail(STATUS_CTX_TOO_LONG);
             }
             co_smem[s + 1] = ctx > 0 ? (ctx + p.split_tokens - 1) / p.split_tokens : 0;
             my_tokens += max(ctx, 0);
@@ -791,7 +801,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
     const int32_t *co = co_in_smem ? co_smem : p.chunk_off_global;
     int32_t n_chunks_total = co[p.n_seqs];
     if (n_chunks_total > p.max_chunks) {  // more chunks than the partials buffer holds: compute nothing, flag it
-        if (blockIdx.x == 0 && tid == 0) raise_status(p.status, STATUS_CTX_TOO_LONG);
+        if (blockIdx.x == 0 && tid == 0) fail(STATUS_CTX_TOO_LONG);
         n_chunks_total = 0;
     }
     const int32_t n_items = n_chunks_total * p.n_kv_heads;
@@ -817,7 +827,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                     if (i > 16) __nanosleep(250);
                 }
                 if (!there) {
-                    raise_status(p.status, STATUS_WAIT_TIMEOUT);
+                    fail(STATUS_WAIT_TIMEOUT);
                     *abort_flag = 1;
                 }
                 if (p.stamps != nullptr && blockIdx.x == 0)
@@ -832,7 +842,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             if (lane == 0) {
                 const uint32_t qs = qn % ATT_QD;
                 if (!mbar_wait(bar_qempty + 8 * qs, ((qn / ATT_QD) & 1u) ^ 1u)) {
-                    raise_status(p.status, STATUS_WAIT_TIMEOUT);
+                    fail(STATUS_WAIT_TIMEOUT);
                     *abort_flag = 1;
                 }
                 if (*abort_flag == 0 && next < n_items) item = next;
@@ -881,11 +891,11 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                         const uint32_t stage = gt % STAGES;
                         const uint32_t phase = (gt / STAGES) & 1u;
                         if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1u)) {
-                            raise_status(p.status, STATUS_WAIT_TIMEOUT);
+                            fail(STATUS_WAIT_TIMEOUT);
                             *abort_flag = 1;
                         }
                         if (sl < 0) {  // unit not on the GPU: flag it, stream slot 0 so the ring stays in step
-                            raise_status(p.status, STATUS_MISSING_UNIT);
+                            fail(STATUS_MISSING_UNIT);
                             sl = 0;
                         }
                         if (*abort_flag == 0) {
@@ -940,7 +950,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
         const uint32_t qs = qn % ATT_QD;
         const bool late = !mbar_wait(bar_qfull + 8 * qs, (qn / ATT_QD) & 1u);
         if (consumer_vote<NCONS>(late || *abort_flag != 0)) {  // uniform: either every consumer goes on or none does
-            if (late) raise_status(p.status, STATUS_WAIT_TIMEOUT);
+            if (late) fail(STATUS_WAIT_TIMEOUT);
             break;
         }
         const int32_t item = q_item[qs];
@@ -996,7 +1006,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             const uint32_t stage = tg % STAGES;
             const uint32_t phase = (tg / STAGES) & 1u;
             if (!mbar_wait(bar_full + 8 * stage, phase)) {
-                raise_status(p.status, STATUS_WAIT_TIMEOUT);
+                fail(STATUS_WAIT_TIMEOUT);
                 *abort_flag = 1;
             }
             __syncwarp();
@@ -1428,6 +1438,8 @@ combine_kernel(const float *part_o, const float *part_ml, const int32_t *chunk_o
 // barrier and in few dependent steps: the scores go into registers while the sequence is looked up (every lane compares some of the
 // chunk offsets), then the weights so far and all heads' maxima and sums (a lane per chunk) are fetched at once.
 // =====================================================================================================
+// A call that raised a status adds nothing: the chunks of a sequence with a block that is not there hold another block's scores, those
+// of a wait that ran out an earlier call's, and sums that took them up could not be put right.  (out can: the call is repeated.)
 constexpr int FIN_THREADS = 128;
 constexpr int FIN_HELD = 16;   // scores that a lane holds
 
@@ -1435,7 +1447,7 @@ template <int D, bool BF16, int G>
 __global__ void __launch_bounds__(FIN_THREADS)
 attn_finish_kernel(const float *scores, const float *part_o, const float *part_ml, const int32_t *chunk_off, const int32_t *ctx_lens,
                    uint16_t *out, float *weights, int64_t stride, int32_t n_seqs, int32_t n_kv_heads, int32_t split_tokens, int32_t max_tokens,
-                   int32_t cap, int32_t slices, int32_t merge_ctas, int32_t *status) {
+                   int32_t cap, int32_t slices, int32_t merge_ctas, int32_t *status, const int32_t *failed, int32_t call) {
     extern __shared__ __align__(16) float comb_smem[];
     constexpr int AHEAD = G >= FIN_HELD ? 1 : FIN_HELD / G;   // tokens of a lane at a time
     grid_launch_dependents();
@@ -1447,6 +1459,7 @@ attn_finish_kernel(const float *scores, const float *part_o, const float *part_m
                                            n_kv_heads * G, n_kv_heads, G, cap);
         return;
     }
+    const bool spoilt = *failed == call;   // (used at the end only: the load is on its way beside the others)
     const int32_t n_items = chunk_off[n_seqs] * n_kv_heads;
     const int32_t pieces = (split_tokens + AHEAD * 32 - 1) / (AHEAD * 32);
     const int32_t weight_ctas = (int32_t)gridDim.x - merge_ctas;
@@ -1515,7 +1528,7 @@ attn_finish_kernel(const float *scores, const float *part_o, const float *part_m
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int32_t t = base + u * 32 + lane;
-            if (t < n) {
+            if (t < n && !spoilt) {
                 float w = 0.f;
 #pragma unroll
                 for (int g = 0; g < G; ++g) w += fast_exp2(v[u][g] - m_all[g]) * inv[g];
@@ -1704,14 +1717,15 @@ cudaError_t attn_weights_configure(int head_dim, int dtype, int *ctas_per_sm, in
     });
 }
 
-int64_t attn_counter_words(int32_t, int32_t) { return 64; }  // [0] next item, [1] CTAs that have left
+int64_t attn_counter_words(int32_t, int32_t) { return 64; }  // three sets of [0] next item, [1] CTAs that have left ...; [ATT_FAILED]
 
 cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const AttnLaunch &a, const CUtensorMap &map,
                              int use3d, cudaStream_t stream) {
     if (a.n_seqs <= 0) return cudaSuccess;
     if (a.n_seqs > ATT_SMEM_SEQS) {  // batch too large for the in-kernel plan: build the chunk offsets first
         plan_kernel<<<1, 1024, 0, stream>>>(a.ctx_lens, a.n_seqs, a.max_blocks * 16, a.split_tokens,
-                                            (int32_t)(sc.max_items / sh.n_kv_heads), sc.chunk_off, a.status);
+                                            (int32_t)(sc.max_items / sh.n_kv_heads), sc.chunk_off, a.status,
+                                            a.weights != nullptr ? sc.counters + ATT_FAILED : nullptr, a.weights_call);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
@@ -1767,6 +1781,8 @@ cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const A
     if (a.k_new == nullptr || a.v_new == nullptr) p.k_new = p.v_new = nullptr;
     if (a.weights != nullptr) {
         p.scores = sc.scores;
+        p.failed = sc.counters + ATT_FAILED;
+        p.call = a.weights_call;
         p.early_trigger = 0;
         cudaError_t ew = dispatch_weights(sh.head_dim, sh.dtype, sh.kv_fp8, [&](auto kernel, int smem, int nw) -> cudaError_t {
             kernel<<<a.grid, (nw + 1) * 32, smem, stream>>>(map, p);
@@ -1795,7 +1811,8 @@ cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const A
         return dispatch_finish(sh.head_dim, sh.dtype, group, [&](auto kernel) {
             return cudaLaunchKernelEx(&lc, kernel, (const float *)sc.scores, (const float *)p.part_o, (const float *)p.part_ml,
                                       (const int32_t *)sc.chunk_off, a.ctx_lens, (uint16_t *)a.out, a.weights, a.weights_stride, a.n_seqs,
-                                      sh.n_kv_heads, a.split_tokens, a.max_blocks * 16, cap, slices, merge_ctas, a.status);
+                                      sh.n_kv_heads, a.split_tokens, a.max_blocks * 16, cap, slices, merge_ctas, a.status, (const int32_t *)p.failed,
+                                      p.call);
         });
     }
     cudaError_t e = dispatch_variant(sh.head_dim, sh.dtype, a.variant, sh.kv_fp8, [&](auto kernel, int smem, int nw) -> cudaError_t {

@@ -162,6 +162,7 @@ struct AttnLaunch {
     // score in the scratch, and the kernel that merges the chunks turns them into weights (the default variant's shape; not deferred).
     float *weights = nullptr;
     int64_t weights_stride = 0;
+    int32_t weights_call = 0;   // a number of its own for every such call on the scratch, not 0
 };
 
 // Build the TMA descriptors of the HBM pool: map3d covers a whole K+V tile in one copy

@@ -141,6 +141,7 @@ struct pie_pool {
     int attn_weights_grid = 0;   // 0: not configured yet
     pie::AttnScratch weights_scratch{};   // the scratch of calls that accumulate weights: room for eight items per CTA at least
     int64_t weights_scores = 0;           // floats of its score buffer
+    uint32_t weights_calls = 0;
     int32_t *evict_scratch = nullptr;   // per kept token its row, per (sequence, KV head) the number of them
     int64_t evict_words = 0;
     int device = 0;
@@ -975,6 +976,8 @@ int attention_call(pie_pool *p, int32_t layer, const void *q, void *out, const i
         a.grid = p->attn_weights_grid;
         a.weights = weights;
         a.weights_stride = weights_stride;
+        if (++p->weights_calls == 0) ++p->weights_calls;
+        a.weights_call = (int32_t)p->weights_calls;
     }
     // a merge the call before this one left: this kernel takes it on if it attends the same batch (else it is merged now)
     if (p->deferred.on && !(dependent && p->deferred.n_seqs == n_seqs && p->deferred.max_blocks == max_blocks && p->deferred.ctx == ctx_dev &&
