@@ -398,8 +398,8 @@ int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out,
  * pools too: the arrays are 16-bit), tokens q_stride / k_stride / v_stride elements apart (0: dense); out: dense, like q.
  * Sequences of any length, empty ones too; rows behind the last offset are left as they were.  What a token may not see
  * cannot reach it, NaN and infinities included.  Scores and sums in fp32, probabilities rounded to the 16-bit type before
- * they meet the values (each by half a step of itself at most, 2^-8 (bf16) or 2^-11 (fp16), independently of the others), out
- * rounded to nearest.
+ * they meet the values (each by half a step of itself at most, 2^-8 (bf16) or 2^-11 (fp16), independently of the others; fp16: or by
+ * 2^-32 of the row's largest probability, if that is more), out rounded to nearest.
  * offsets_host: host, n_seqs + 1 entries, first 0, ascending; read before the call returns.  PIE_ERR_INVALID: offsets that are
  * not, pointers or strides not on a 16-byte boundary, a stride below its row, out overlapping an input, more than 131072 pieces
  * of 256 / (n_q_heads / n_kv_heads) tokens (an even number, counted per sequence) in one call of a small pool.  PIE_ERR_UNSUPPORTED while the

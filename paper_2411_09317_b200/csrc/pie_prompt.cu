@@ -54,6 +54,12 @@ constexpr int PR_TMEM_COLS = 512;             // S0, S1 (128 each; P over them),
 // units): probabilities are then at most 2^8, harmless in fp32 sums and in both 16-bit types, and after the first stages
 // hardly any stage rescales.
 constexpr float PR_LAZY = 8.f;
+// fp16 has only subnormal numbers below 2^-14 and none below 2^-24: beside one dominating key thousands of small probabilities
+// would lose bits, or all of them, while the row's sum counts them.  For fp16 the running maximum is therefore kept less 7, and all
+// probabilities are 2^7 as large (2^15 at most; O and the sum carry the factor, which cancels): what one loses below fp16's smallest
+// step is then at most 2^-32 of the row's largest probability.  (As long as before where no P was lost; where many were zero the
+// products of zeros had taken less power: 10007 tokens, 32 / 8 heads of 128, scores of N(0, 4^2): 795 -> 831 us.)
+constexpr float PR_SHIFT_F16 = 15.f - PR_LAZY;
 
 constexpr int PR_INLINE = 480;   // items that travel with the launch's parameters (7.5 KiB): no copy in front of the call.  It saves 7 us
                                  // (16 ragged prompts: 135 -> 128 us); with 960 a call of 45 tokens takes 0.5 us longer, with 1900 1.8 us
@@ -517,7 +523,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 a2 = pr_max3(a2, __uint_as_float(sv[2][c]), __uint_as_float(sv[2][c + 1]));
                 a3 = pr_max3(a3, __uint_as_float(sv[3][c]), __uint_as_float(sv[3][c + 1]));
             }
-            const float mx = pr_max3(a0, a1, pr_max3(a2, a3, a3)) * scale;
+            const float mx = pr_max3(a0, a1, pr_max3(a2, a3, a3)) * scale - (BF16 ? 0.f : PR_SHIFT_F16);
             spoiled |= !(mx < INFINITY);
             const float m_cand = fmaxf(m_run, mx);
             const bool grow = m_cand > m_run + PR_LAZY;               // (m_run = -inf: true unless the row has seen nothing finite yet)

@@ -85,3 +85,44 @@ def test_weights_of_a_call_with_a_context_beyond_its_table_stay_as_they_were(seq
         c.call()
         pie.pie_sync(p.h)
         c.check()
+
+
+# ================================================================================== rows that one key dominates (fp16 range)
+def sink_rows(seed, n, hq, hkv, d, dtype, nats, at):
+    """q, k, v bits and the scale: the key at `at` lies `nats` (give or take a half) above all others, and its value is 0."""
+    rng = np.random.default_rng(seed)
+    q, k = np.zeros((n, hq, d)), np.zeros((n, hkv, d))
+    q[:, :, 0] = 8.0
+    k[:, :, 0] = rng.uniform(-1.0, 1.0, (n, hkv))
+    k[at, :, 0] = 2.0 * nats
+    k[:, :, 1:] = rng.standard_normal((n, hkv, d - 1))
+    bits = lambda x: synth.f32_to_16_bits(x.astype(np.float32), dtype)  # noqa: E731
+    v = np.abs(rng.standard_normal((n, hkv, d)))
+    v[at] = 0.0
+    return bits(q), bits(k), bits(v), 1.0 / 16
+
+
+def sink_bound(dtype, want, size, weights, v, below):
+    """As check_prompt, and for P in fp16 what a probability may lose below the type's smallest step: `below` of the largest."""
+    u, tiny = (2.0 ** -11, 2.0 ** -25) if dtype == F16 else (2.0 ** -8, 2.0 ** -134)
+    return (u + 4e-4) * size + u * np.abs(want) + tiny + below * weights.max() * np.abs(v).sum(axis=0)
+
+
+@pytest.mark.parametrize("d,dtype", [(128, F16), (64, F16), (128, BF16)])
+@pytest.mark.parametrize("nats,at", [(5.5, 200), (12.0, 0), (14.0, 0), (16.0, 0), (16.0, 131), (17.4, 0), (18.5, 0), (17.4, 4000)])
+def test_prompt_rows_that_one_key_dominates(d, dtype, nats, at):
+    """Thousands of keys far below one whose value is 0: what they add up to is the whole output."""
+    n, hq, hkv = 4001, 4, 2
+    q, k, v, scale = sink_rows(900, n, hq, hkv, d, dtype, nats, at)
+    dq, dk, dv = up(q), up(k), up(v)
+    out = torch.zeros_like(dq)
+    with Pool(hq, hkv, d, dtype, 1) as p:
+        pie.pie_prompt_attention(p.h, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), out.data_ptr(), np.array([0, n], np.int32), 1, scale)
+        pie.pie_sync(p.h)
+    q, k, v, got = real(q, dtype), real(k, dtype), real(v, dtype), down(out, dtype)
+    for i in [0, 1, at, 127, 128, 300, 1000, 2047, 3000, n - 1]:
+        for h in range(hq):
+            want, w, size = oo.attend(q[i, h], k[:i + 1, h // 2], v[:i + 1, h // 2], scale)
+            bound = sink_bound(dtype, want, size, w, v[:i + 1, h // 2], 2.0 ** -32 if dtype == F16 else 0.0)
+            err = np.abs(got[i, h] - want)
+            assert np.all(err <= bound), (i, h, float((err / bound).max()))
