@@ -441,6 +441,10 @@ cudaError_t launch_swap_bulk(const void *src_pool, void *dst_pool, const int32_t
 // timing, so a run with swapped blocks reproduces a resident run bit for bit.
 // All waits are bounded: a wait that runs out raises a status word and the CTA leaves through its barriers.
 // =====================================================================================================
+// Where the products run in fp16, whose numbers below 2^-14 are subnormal and below 2^-24 none, the probabilities (1 at most) are
+// multiplied by this on their way there, and the item's output by its inverse: thousands of small ones beside one dominating key
+// keep their bits (to 2^-40 of the largest).  A power of two, so nothing else changes.
+constexpr float ATT_P_SCALE_F16 = 32768.f;
 constexpr int ATT_QD = 2;           // depth of the producer -> consumer item queue (item id + its query rows)
 constexpr int ATT_FAILED = 32;      // the counters' word that holds the number of the last weights call that raised a status
 constexpr int ATT_SMEM_SEQS = 1024; // largest batch whose chunk offsets are built in shared memory
@@ -485,7 +489,7 @@ struct AttnParams {
     int64_t n_gpu_slots;
     int32_t max_blocks, n_seqs, n_q_heads, n_kv_heads, group, n_logical, split_tokens, use3d, max_chunks;
     float scale_log2e;      // softmax scale * log2(e) (* the key scale of an 8-bit pool)
-    float out_scale = 1.f;  // 8-bit pools: the value scale (times what the kernel's 16-bit images of the bytes leave out)
+    float out_scale = 1.f;  // 1 / ATT_P_SCALE_F16 where the products run in fp16; 8-bit pools: times the value scale
     float k_scale = 1.f, v_scale = 1.f;  // 8-bit pools: the append stores E4M3(x / scale)
     // Calls that accumulate attention weights (instantiations with SCORES): every valid token's scores, in log2 units, as
     // [item][token of the chunk][head of the group] - see attn_finish_kernel.
@@ -1176,7 +1180,8 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                 }
             }
             // P^T as the B operand of O^T += V^T P^T: transpose the two 8x8 (token x head) blocks
-            const uint32_t h01 = pack2<MB>(p0, p1), h23 = pack2<MB>(p2, p3);
+            constexpr float P_SCALE = MB ? 1.f : ATT_P_SCALE_F16;
+            const uint32_t h01 = pack2<MB>(p0 * P_SCALE, p1 * P_SCALE), h23 = pack2<MB>(p2 * P_SCALE, p3 * P_SCALE);
             const uint32_t pb0 = movmatrix_trans(h01);
             const uint32_t pb1 = movmatrix_trans(h23);
             // bf16 keeps 8 significant bits: carry the rounding remainder of P in a second bf16 term so that the
@@ -1280,7 +1285,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                 acc += mo[(w * 8 + g) * SM::MO_STRIDE + d] * wt;
                 ll += ml[(w * 8 + g) * 2 + 1] * wt;
             }
-            acc *= p.out_scale;  // 1 for 16-bit pools
+            acc *= p.out_scale;
             if (it.nchunks == 1) {
                 // the whole context in one chunk: normalise and round here
                 const float r = acc * (ll > 0.f ? 1.f / ll : 0.f);
@@ -1778,6 +1783,7 @@ cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const A
         p.v_scale = p.out_scale = a.v_scale;
         p.scale_log2e *= a.k_scale;  // scores over the stored keys are scores over the keys / k_scale
     }
+    if (sh.kv_fp8 || sh.dtype != PIE_BF16) p.out_scale *= 1.f / ATT_P_SCALE_F16;
     if (a.k_new == nullptr || a.v_new == nullptr) p.k_new = p.v_new = nullptr;
     if (a.weights != nullptr) {
         p.scores = sc.scores;

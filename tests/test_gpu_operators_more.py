@@ -126,3 +126,38 @@ def test_prompt_rows_that_one_key_dominates(d, dtype, nats, at):
             bound = sink_bound(dtype, want, size, w, v[:i + 1, h // 2], 2.0 ** -32 if dtype == F16 else 0.0)
             err = np.abs(got[i, h] - want)
             assert np.all(err <= bound), (i, h, float((err / bound).max()))
+
+
+def e4m3_bytes(x):
+    return torch.from_numpy(x.astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+
+
+@pytest.mark.parametrize("d,dtype,fp8", [(128, F16, False), (64, F16, False), (128, BF16, False), (128, F16, True), (128, BF16, True)])
+@pytest.mark.parametrize("nats,at", [(12.0, 0), (15.0, 700), (17.4, 0), (19.0, 1)])
+def test_decode_rows_that_one_key_dominates(d, dtype, fp8, nats, at):
+    """The same from the cache, with and without weights; P (1 at most) is scaled by 2^15, so that half of fp16's smallest step is
+    2^-40 of the largest probability."""
+    n, hq, hkv = 1000, 4, 2
+    q, k, v, scale = sink_rows(910, n, hq, hkv, d, dtype, nats, at)
+    q = q[:1]
+    with Pool(hq, hkv, d, dtype, (n + 15) // 16, fp8=fp8, seqs=1, split_tokens=1024) as p:
+        kv = np.zeros((p.blocks * 16, hkv, 2, d), np.uint8 if fp8 else np.uint16)
+        for i, x in enumerate((k, v)):
+            kv[:n, :, i] = e4m3_bytes(real(x, dtype) / p.scales[i]) if fp8 else x
+        data = np.ascontiguousarray(kv.reshape(p.blocks, 16, hkv, 2, d).transpose(0, 2, 3, 1, 4))
+        p.fill(data)
+        tab, ctx, dq = up(np.arange(p.blocks, dtype=np.int32)[None]), up(np.array([n], np.int32)), up(q)
+        w, outs = torch.zeros((1, hkv, n), dtype=torch.float32, device=DEV), [torch.zeros_like(dq) for _ in range(2)]
+        args = (tab.data_ptr(), p.blocks, ctx.data_ptr())
+        pie.pie_decode_attention_weights(p.h, 0, dq.data_ptr(), outs[0].data_ptr(), *args, 1, scale, w.data_ptr(), n)
+        pie.pie_decode_attention(p.h, 0, dq.data_ptr(), outs[1].data_ptr(), *args, 1, scale)
+        pie.pie_sync(p.h)
+        assert torch.equal(outs[0], outs[1])
+        stored = p.values(data).transpose(0, 3, 1, 2, 4).reshape(-1, hkv, 2, d)[:n]
+    want_w = oo.attention_weights(real(q[0], dtype), stored[:, :, 0], scale)
+    assert np.all(np.abs(w[0].cpu().numpy() - want_w) <= 1.3e-4 * want_w + 1e-30)
+    for h in range(hq):
+        want, weights, size = oo.attend(real(q[0, h], dtype), stored[:, h // 2, 0], stored[:, h // 2, 1], scale)
+        bound = sink_bound(dtype, want, size, weights, stored[:, h // 2, 1], 2.0 ** -40 if fp8 or dtype == F16 else 0.0)
+        err = np.abs(down(outs[0][0, h], dtype) - want)
+        assert np.all(err <= bound), (h, float((err / bound).max()))
