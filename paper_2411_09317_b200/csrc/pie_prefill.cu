@@ -49,6 +49,9 @@ constexpr int PF_TMEM_COLS = 256;
 // are taken against the older maximum and may reach 2^8, which fp32 sums and both 16-bit types hold without loss.  With
 // an exact running maximum some row of a warp moves its maximum in most stages, even hundreds of stages in.
 constexpr float PF_LAZY = 8.f;
+// fp16 pools: the running maximum is kept less this, so that every probability is 2^7 as large (2^15 at most; O and the sum carry the
+// factor, which cancels) and thousands of small ones beside one dominating key do not fall below fp16's smallest numbers, 2^-24.
+constexpr float PF_SHIFT_F16 = 15.f - PF_LAZY;
 
 struct PrefillParams {
     const uint16_t *q;
@@ -758,7 +761,7 @@ prefill_attn_wide_kernel(const __grid_constant__ CUtensorMap tmap, const Prefill
                     }
                 }
             }
-            const float m_cand = fmaxf(m_run, mx);
+            const float m_cand = fmaxf(m_run, mx - (BF16 ? 0.f : PF_SHIFT_F16));
             const bool grow = m_cand > m_run + PF_LAZY;   // (m_run = -inf: true unless the row has seen nothing yet)
             const float m_new = grow ? m_cand : m_run;
             const float alpha = grow ? pf_exp2(m_run - m_cand) : 1.f;   // (m_run = -inf gives 0: nothing accumulated yet)

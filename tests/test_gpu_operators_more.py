@@ -161,3 +161,30 @@ def test_decode_rows_that_one_key_dominates(d, dtype, fp8, nats, at):
         bound = sink_bound(dtype, want, size, weights, stored[:, h // 2, 1], 2.0 ** -40 if fp8 or dtype == F16 else 0.0)
         err = np.abs(down(outs[0][0, h], dtype) - want)
         assert np.all(err <= bound), (h, float((err / bound).max()))
+
+
+@pytest.mark.parametrize("d,dtype", [(128, F16), (64, F16), (128, BF16)])
+@pytest.mark.parametrize("nats,at", [(5.5, 200), (12.0, 0), (16.0, 300), (17.4, 0), (17.4, 999)])
+def test_chunk_rows_that_one_key_dominates(d, dtype, nats, at):
+    """The same for a chunk of 70 tokens at the end of 1000 cached ones (P up to 2^15 in fp16, as for whole prompts)."""
+    n, chunk, hq, hkv = 1000, 70, 4, 2
+    q, k, v, scale = sink_rows(920, n, hq, hkv, d, dtype, nats, at)
+    q = q[n - chunk:]
+    with Pool(hq, hkv, d, dtype, (n + 15) // 16, seqs=1) as p:
+        kv = np.zeros((p.blocks * 16, hkv, 2, d), np.uint16)
+        kv[:n, :, 0], kv[:n, :, 1] = k, v
+        p.fill(np.ascontiguousarray(kv.reshape(p.blocks, 16, hkv, 2, d).transpose(0, 2, 3, 1, 4)))
+        tab, lens, off = np.arange(p.blocks, dtype=np.int32)[None], np.array([n], np.int32), np.array([0, chunk], np.int32)
+        dtab, dlens, doff, dq = up(tab), up(lens), up(off), up(q)
+        out = torch.zeros_like(dq)
+        pie.pie_prefill_attention(p.h, 0, dq.data_ptr(), out.data_ptr(), dtab.data_ptr(), p.blocks, dlens.data_ptr(), doff.data_ptr(), lens, off, 1,
+                                  scale)
+        pie.pie_sync(p.h)
+    q, k, v, got = real(q, dtype), real(k, dtype), real(v, dtype), down(out, dtype)
+    for i in [0, 1, 33, chunk - 1]:
+        m = n - chunk + i + 1
+        for h in range(hq):
+            want, w, size = oo.attend(q[i, h], k[:m, h // 2], v[:m, h // 2], scale)
+            err = np.abs(got[i, h] - want)
+            bound = sink_bound(dtype, want, size, w, v[:m, h // 2], 2.0 ** -32 if dtype == F16 else 0.0)
+            assert np.all(err <= bound), (i, h, float((err / bound).max()))
