@@ -39,6 +39,9 @@ class WeightsCase:
     def check(self, steps=1):
         got, kv, p = self.w.cpu().numpy().astype(np.float64), self.p.values(self.data), self.p
         for s, n in enumerate(self.lens):
+            if n == 0:
+                assert not down(self.out[s], p.dtype).any() and np.array_equal(got[s], self.before[s].astype(np.float64))
+                continue
             ids = self.table[s, :(n + 15) // 16]
             k, v = (kv[ids, :, i].transpose(0, 2, 1, 3).reshape(-1, p.hkv, p.d)[:n] for i in (0, 1))
             added = steps * oo.attention_weights(real(self.q[s], p.dtype), k, self.scale)
@@ -188,3 +191,77 @@ def test_chunk_rows_that_one_key_dominates(d, dtype, nats, at):
             err = np.abs(got[i, h] - want)
             bound = sink_bound(dtype, want, size, w, v[:m, h // 2], 2.0 ** -32 if dtype == F16 else 0.0)
             assert np.all(err <= bound), (i, h, float((err / bound).max()))
+
+
+# ============================================================================== tables and strides much wider than the batch
+@pytest.mark.parametrize("hq,hkv,d,dtype,fp8", [(8, 2, 64, F16, False), (8, 8, 128, BF16, False), (4, 1, 128, F16, True)])
+@pytest.mark.parametrize("lens,width", [([333], 2048), ([1, 700, 0, 45], 2048), ([50] * 9, 8000)])
+def test_weights_of_short_sequences_in_a_wide_table(hq, hkv, d, dtype, fp8, lens, width):
+    """The table and the rows of the account are made for 32 768 tokens and more; entries behind a sequence's blocks name no block."""
+    with Pool(hq, hkv, d, dtype, sum((n + 15) // 16 for n in lens), fp8=fp8) as p:
+        c = WeightsCase(p, lens, 830, width=width, spare=16 * width)
+        c.call()
+        c.call()
+        pie.pie_sync(p.h)
+        c.check(steps=2)
+
+
+class EvictCase:
+    """One eviction of random blocks, weights as given, into wider tables and strides; check() against the oracle's choice."""
+
+    def __init__(self, p, lens, w, budget, recent, in_place, seed, width=None):
+        self.p, self.lens, self.w, self.in_place = p, lens, w, in_place
+        need = sum((n + 15) // 16 for n in lens)
+        data = p.random(seed)
+        p.fill(data)
+        table = table_for(lens, need, seed, width)
+        dst = table if in_place else table_for([min(n, budget) for n in lens], p.blocks - need, seed + 1, width, first=need)
+        dt, dd, dw, ctx = up(table), up(dst), up(w), up(np.array(lens, np.int32))
+        out = dw if in_place else torch.full(w.shape, -7.0, dtype=torch.float32, device=DEV)
+        kept = torch.full((len(lens), p.hkv, budget), 12345, dtype=torch.int32, device=DEV)
+        pie.pie_kv_evict(p.h, 0, dt.data_ptr(), table.shape[1], ctx.data_ptr(), len(lens), dw.data_ptr(), w.shape[2], budget, recent,
+                         dst_block_table_dev=None if in_place else dd.data_ptr(), dst_max_blocks=0 if in_place else dst.shape[1],
+                         weights_out=None if in_place else out.data_ptr(), weights_out_stride=0 if in_place else w.shape[2],
+                         new_lens_dev=ctx.data_ptr(), kept_dev=kept.data_ptr())
+        pie.pie_sync(p.h)
+        want, want_w = data.copy(), w.copy() if in_place else np.full(w.shape, -7.0, np.float32)
+        got_k = kept.cpu().numpy()
+        for s, n in enumerate(lens):
+            m = min(n, budget)
+            for h in range(p.hkv):
+                chosen = oo.keep(w[s, h], n, budget, recent)
+                assert got_k[s, h].tolist() == chosen + [-1] * (budget - m), (s, h)
+                to, c = np.arange(m), np.array(chosen, np.int64)
+                want[dst[s, to // 16], h, :, to % 16] = data[table[s, c // 16], h, :, c % 16]
+                want_w[s, h, :m], want_w[s, h, m:n] = w[s, h, c], 0.0
+        assert np.array_equal(p.raw(), want)
+        assert np.array_equal(out.cpu().numpy().view(np.uint32), want_w.view(np.uint32))
+        assert ctx.cpu().numpy().tolist() == [min(n, budget) for n in lens]
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lens,width,budget", [([700], 2048, 100), ([333, 20, 0, 1200], 7500, 90)])
+def test_evict_short_sequences_in_a_wide_table(in_place, fp8, lens, width, budget):
+    """2048 blocks a row: sixteen weights a thread for a short sequence; 7500: the blocks' slots are looked up again."""
+    blocks = sum((n + 15) // 16 + (min(n, budget) + 15) // 16 for n in lens)
+    with Pool(4, 2, 128, F16, blocks, fp8=fp8) as p:
+        w = np.exp(2 * np.random.default_rng(6).standard_normal((len(lens), 2, 16 * width))).astype(np.float32)
+        EvictCase(p, lens, w, budget, 11, in_place, 340, width=width)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("name", ["zeros", "few values", "odd", "rising", "falling", "close"])
+@pytest.mark.parametrize("budget,recent", [(600, 100), (9000, 0), (17000, 300)])
+def test_evict_selection_over_several_pieces(in_place, name, budget, recent):
+    """20 000 tokens, more than the selecting threads hold at a time, with hundreds of weights that share the first digits or are
+    equal: all digits are searched, and the places left for equal weights end in the first, second or third piece."""
+    n, hkv = 20000, 2
+    rng, shape = np.random.default_rng(9), (1, hkv, n + 3)
+    t = np.arange(n + 3)
+    w = {"zeros": np.zeros(shape), "few values": rng.integers(0, 3, shape) * 1.5,
+         "odd": rng.choice([0.0, -0.0, np.nan, np.inf, -np.inf, 1.0, -1.0, 1e-40], shape),
+         "rising": np.broadcast_to(1 + t * 2.0 ** -23, shape), "falling": np.broadcast_to(2 - t * 2.0 ** -23, shape),
+         "close": 1 + rng.integers(0, 5000, shape) * 2.0 ** -23}[name]
+    with Pool(2, hkv, 64, F16, 1250 + (budget + 15) // 16, seqs=1) as p:
+        EvictCase(p, [n], np.ascontiguousarray(w, dtype=np.float32), budget, recent, in_place, 350)
