@@ -1537,7 +1537,10 @@ attn_finish_kernel(const float *scores, const float *part_o, const float *part_m
                 float w = 0.f;
 #pragma unroll
                 for (int g = 0; g < G; ++g) w += fast_exp2(v[u][g] - m_all[g]) * inv[g];
-                wrow[t] = old[u] + w;
+                // (not by +, which the library's flags make flush a subnormal sum: a decayed account keeps its order)
+                float sum;
+                asm("add.rn.f32 %0, %1, %2;" : "=f"(sum) : "f"(old[u]), "f"(w));
+                wrow[t] = sum;
             }
         }
     }

@@ -90,6 +90,26 @@ def test_weights_of_a_call_with_a_context_beyond_its_table_stay_as_they_were(seq
         c.check()
 
 
+@pytest.mark.parametrize("d,dtype", [(64, F16), (128, BF16)])
+def test_weights_keep_what_a_decayed_account_holds(d, dtype):
+    """Sums that have decayed to subnormal numbers, of tokens whose probability is below 2^-126 (a key 200 nats above them): 0 is added
+    and every bit stays, by which an eviction still tells them apart."""
+    n, hq, hkv = 70, 4, 2
+    with Pool(hq, hkv, d, dtype, (n + 15) // 16, seqs=1) as p:
+        q, k, v, scale = sink_rows(930, n, hq, hkv, d, dtype, 200.0, 20)
+        kv = np.zeros((p.blocks * 16, hkv, 2, d), np.uint16)
+        kv[:n, :, 0], kv[:n, :, 1] = k, v
+        p.fill(np.ascontiguousarray(kv.reshape(p.blocks, 16, hkv, 2, d).transpose(0, 2, 3, 1, 4)))
+        before = (np.arange(hkv * n).reshape(1, hkv, n) * 2.0 ** -149).astype(np.float32)
+        tab, ctx, dq, w = up(np.arange(p.blocks, dtype=np.int32)[None]), up(np.array([n], np.int32)), up(q[:1]), up(before)
+        out = torch.zeros_like(dq)
+        pie.pie_decode_attention_weights(p.h, 0, dq.data_ptr(), out.data_ptr(), tab.data_ptr(), p.blocks, ctx.data_ptr(), 1, scale, w.data_ptr(), n)
+        pie.pie_sync(p.h)
+    got, others = w.cpu().numpy(), np.arange(n) != 20
+    assert np.array_equal(got[:, :, others].view(np.uint32), before[:, :, others].view(np.uint32))
+    assert np.all(np.abs(got[:, :, 20] - hq / hkv) <= 1.3e-4 * hq / hkv)
+
+
 # ================================================================================== rows that one key dominates (fp16 range)
 def sink_rows(seed, n, hq, hkv, d, dtype, nats, at):
     """q, k, v bits and the scale: the key at `at` lies `nats` (give or take a half) above all others, and its value is 0."""
