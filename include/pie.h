@@ -355,7 +355,8 @@ int pie_prefill_attention(pie_pool *pool, int32_t layer, const void *q, void *ou
  * pair_axis, inv_freq: host, rotary_dim / 2 entries each; axes are 0 .. 3, and a call's positions have one row per axis up
  * to the largest one named.  Frequencies are radians per position (their own scaling for long contexts included), amplitude
  * what such schemes multiply the cosine and the sine by (1 otherwise).  Angles are formed in 64-bit fixed point, in turns:
- * a position of any size, negative ones too, keeps its fraction to 2^-32 of a turn.
+ * a position of any size, negative ones too, keeps its fraction to 2^-32 of a turn, which is then rounded to fp32 for the sine and
+ * the cosine (by 2^-26 of a turn at most, 9.4e-8 radians).
  * Can be called again at any time; calls already enqueued keep the setting they were made with.
  * PIE_ERR_INVALID: a null pointer, an axis outside 0 .. 3, a frequency or amplitude that is not finite, amplitude <= 0,
  * rotary_dim <= 0 or above head_dim.  PIE_ERR_UNSUPPORTED: rotary_dim not a multiple of 16. */
@@ -369,8 +370,8 @@ int pie_rope_plan(int32_t head_dim, int32_t rotary_dim, const int32_t *pair_axis
                   int32_t *n_axes);
 /* Rotates q and k of n_tokens tokens and writes the rotated k and v into the cache, as pie_kv_write does, in one pass:
  *   q [n_tokens][n_q_heads][head_dim] -> q_out, k [n_tokens][n_kv_heads][head_dim] -> the cache and, if k_out is not NULL,
- *   k_out; v (as k) -> the cache.  All in the pool's 16-bit type; the rotation is computed in fp32 and rounded once (an 8-bit
- *   cache takes E4M3(rotated value / scale) straight from fp32).
+ *   k_out; v (as k) -> the cache.  All in the pool's 16-bit type; the rotation is computed in fp32 (numbers
+ *   below 2^-126 count as 0) and rounded once (an 8-bit cache takes E4M3(rotated value / scale) straight from fp32).
  * q_stride, k_stride, v_stride: elements from a token to the next (0: dense); q, k and v may be slices of one projection's
  * rows.  q_out and k_out are dense and may be q and k themselves where those are dense.
  * positions_dev: device int32 [n_axes][n_tokens].  token_seq_dev, token_pos_dev, block_table_dev: as for pie_kv_write - the
@@ -391,7 +392,8 @@ int pie_rope_kv_write(pie_pool *pool, int32_t layer, const void *q, void *q_out,
 
 /* ---- attention over whole prompts (Section 2.1: the prefill stage computes all prompt tokens at once) ---------------
  * For prompts with nothing cached before them: keys and values are read from k and v as the projection left them, the cache
- * is not touched (pie_kv_write or pie_rope_kv_write fills it, before or after).  Sequence s owns tokens offsets_host[s] ..
+ * is not touched (pie_kv_write or pie_rope_kv_write fills it, before or after).  No attention weights come out: the account that
+ * pie_kv_evict goes by starts with the first pie_decode_attention_weights behind the prompt.  Sequence s owns tokens offsets_host[s] ..
  * offsets_host[s + 1] - 1 of the packed arrays and each of its tokens attends to its sequence's tokens up to itself:
  *     out[i][h] = sum_{t <= i} softmax_t(scale * q[i][h] . k[t][kvh]) * v[t][kvh],    kvh = h / (n_q_heads / n_kv_heads)
  * q: device [n_tokens][n_q_heads][head_dim], k, v: device [n_tokens][n_kv_heads][head_dim] in the pool's 16-bit type (8-bit

@@ -328,7 +328,8 @@ __device__ __forceinline__ void write_new_len(const EvictParams &p, int32_t pair
 // Out of place: a CTA copies MOVE_ROWS consecutive rows of K and V.  The rows' places go through shared memory first, so that the
 // chain of dependent look-ups (row, block, slot) is walked once per 128 rows and the copies behind it are independent loads,
 // eight in flight per thread.  The moved rows are written to make room for reads (streaming stores): 240 -> 225 us for 1024 of 4096
-// tokens, 32 x 32 pairs (1.1 GB), 27 -> 23 us for 24 sequences of 8-bit rows.
+// tokens, 32 x 32 pairs (1.1 GB), 27 -> 23 us for 24 sequences of 8-bit rows called back to back, which leaves them in L2 (33 us with
+// rows that come from HBM).
 template <int VECS>
 __global__ void __launch_bounds__(MOVE_THREADS, 5)
 evict_copy_kernel(const EvictParams p, int32_t chunks) {
@@ -374,6 +375,8 @@ evict_copy_kernel(const EvictParams p, int32_t chunks) {
 // several CTAs; slices do not meet, which keeps the move safe without any order between CTAs.  Row j comes from a row at or behind
 // j, in ascending order: what a batch overwrites lies in front of everything that later batches read, so it is enough that a
 // batch has been read by all threads before any of it is written (one barrier), and the next batch may be read ahead of that.
+// 1024 of 4096 tokens, 32 x 32 pairs, 16 bits: 456 us, twice the move out of place; 24 sequences of 8-bit rows 42 us (36): every
+// slice walks the look-ups (row, block, slot) of all rows again, and a batch is 256 rows.
 __global__ void __launch_bounds__(MOVE_THREADS)
 evict_move_kernel(const EvictParams p, int32_t slice_vecs) {
     const EvictLaunch &a = p.a;
@@ -451,7 +454,8 @@ cudaError_t launch_evict(const AttnShape &sh, const EvictLaunch &a, cudaStream_t
     p.row_vecs = sh.head_dim * (sh.kv_fp8 ? 1 : 2) / 16;
     const int64_t pairs = (int64_t)a.n_seqs * sh.n_kv_heads;
     // weights in registers as far as the longest sequence that the table and the weights allow.  The selection takes, with 2, 8 and
-    // 16 weights a thread: one sequence of 700 tokens 7.0, 7.8, 9.2 us; 24 of up to 3500 -, 11.2, 13.8; 32 of 4096 -, 30, 42
+    // 16 weights a thread: one sequence of 700 tokens 7.0, 7.8, 9.2 us; 24 of up to 3500 -, 11.2, 13.8; 32 of 4096 -, 30, 42.  (The
+    // lengths are on the device: a table and weights for 32768 tokens cost short sequences 2 to 4 us, 13.3 -> 17.4 for one of 700.)
     const int64_t longest = std::min<int64_t>((int64_t)a.max_blocks * 16, a.weights_stride);
     const int32_t smem_slots = a.max_blocks <= SEL_SLOTS ? 1 : 0;
     const size_t smem = smem_slots ? (size_t)a.max_blocks * 4 : 0;

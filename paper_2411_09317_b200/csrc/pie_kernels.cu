@@ -1185,7 +1185,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             const uint32_t pb0 = movmatrix_trans(h01);
             const uint32_t pb1 = movmatrix_trans(h23);
             // bf16 keeps 8 significant bits: carry the rounding remainder of P in a second bf16 term so that the
-            // PV product sees ~16 bits (fp16's 11 bits need no correction)
+            // PV product sees ~16 bits (fp16's 11 bits need no correction, its range does: P_SCALE)
             uint32_t pl0 = 0, pl1 = 0;
             if (MB) {
                 pl0 = movmatrix_trans(pack2<true>(p0 - __uint_as_float(h01 << 16), p1 - __uint_as_float(h01 & 0xffff0000u)));

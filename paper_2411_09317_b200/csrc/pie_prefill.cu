@@ -767,7 +767,8 @@ prefill_attn_wide_kernel(const __grid_constant__ CUtensorMap tmap, const Prefill
             const float alpha = grow ? pf_exp2(m_run - m_cand) : 1.f;   // (m_run = -inf gives 0: nothing accumulated yet)
             // ---- second pass: P in the 16-bit type, two tokens per 32-bit word: the A operand of O += P V, kept in tensor
             // memory where the half's scores were.  bf16 keeps 8 significant bits: the rounding remainder of P goes into a
-            // second bf16 operand, so that the product sees about 16 bits (fp16's 11 bits need no correction).
+            // second bf16 operand, so that the product sees about 16 bits (fp16's 11 bits need no correction, its range
+            // does: PF_SHIFT_F16).
             float sum = 0.f;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {

@@ -22,7 +22,9 @@
 // scores is longer than the other tile covers) and, under load, the power limit.  Two score buffers of 64 columns per tile, which
 // cut the chain, lose more: a product of 64 columns takes as long as one of 128 (782 us against 638).  One prompt of 10007 tokens,
 // 32 / 8 heads of 128, bf16: 636 us, 1290 TFLOP/s (half a second of it: 750 us at 1.63 GHz); 16 ragged prompts of 12112 tokens:
-// 124 us; 32 of 512: 108 us; 45 tokens: 7 us, most of it the host's.  Short prompts pay 1.4 us per item for the epilogue, whose
+// 124 us called back to back, which leaves their arrays in L2, and 149 with arrays that come from HBM; 32 of 512: 108 us (back to
+// back); heads of 64, fp16, one prompt of 10007 tokens: 545 us, 566 from HBM (half a stage's products, all of its exponentials: the
+// special-function unit alone takes 2048 cycles a stage, 356 us in all); 45 tokens: 7 us, most of it the host's.  Short prompts pay 1.4 us per item for the epilogue, whose
 // stores take a line per lane: exchanging sectors between two lanes or four first costs as much as it saves (128 and 130 us for the
 // ragged prompts, then at 129).
 // Scores and sums in fp32.  P is rounded once to the 16-bit type on its way to the tensor core (a second operand with the
@@ -158,9 +160,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     constexpr int HALVES = D / 64;
     constexpr int RING = SM::RING;
     // (All exponentials in the special-function unit, 16 a clock and SM: as long for a stage's as the tensor core for its products.
-    // An eighth, a quarter, three eighths of them by a polynomial in the arithmetic pipes cost as many instructions as that relief
-    // gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128: 0, 1, 2, 3 eighths 649, 653, 654, 685 us; 16 ragged prompts:
-    // 127, 127, 128, 149 us; heads of 64: 585, 594, 564, 619 us.)
+    // An eighth, a quarter, three eighths of them by a polynomial in the arithmetic pipes cost heads of 128 as many instructions as
+    // that relief gives back.  One prompt of 10007 tokens, 32 / 8 heads of 128, bf16: 0, 1, 2, 3 eighths 649, 653, 654, 685 us; 16
+    // ragged prompts: 127, 127, 128, 149 us.  Heads of 64, fp16, 10007 tokens, the kernel as it was then: 585, 594, 564, 619 us - a
+    // quarter gained 4 % there; one form was kept for both.)
     extern __shared__ __align__(1024) uint8_t pr_smem[];
     uint8_t *smem = pr_smem;
     const uint32_t base = pf_smem_u32(pr_smem);

@@ -1,9 +1,9 @@
 // Rotary positions of several axes (time, height, width ...) fused with the write into the paged cache.
 //
 // A token's pair i turns by positions[axis(i)][token] * f_i.  The frequencies come as 2^64-ths of a turn per position, so the
-// angle is one 64-bit integer product whose low word IS the fraction of a turn: nothing is lost at far positions (an fp32
+// angle is one 64-bit integer product whose low word IS the fraction of a turn: far positions lose nothing (an fp32
 // product has no fraction left at 2^24 radians and is off by 0.06 at a million), and no range reduction is needed before
-// sincospif.
+// sincospif, whose fp32 argument is off by 2^-26 of a turn at most.
 //
 // The work is moving bytes: q, k and v are read once, q_out, k_out and the cache rows written once.  A CTA takes T consecutive
 // tokens.  It first puts the cosines and sines of its tokens' pairs into shared memory - all heads share them, and evaluating
