@@ -489,7 +489,7 @@ struct AttnParams {
     int64_t n_gpu_slots;
     int32_t max_blocks, n_seqs, n_q_heads, n_kv_heads, group, n_logical, split_tokens, use3d, max_chunks;
     float scale_log2e;      // softmax scale * log2(e) (* the key scale of an 8-bit pool)
-    float out_scale = 1.f;  // 1 / ATT_P_SCALE_F16 where the products run in fp16; 8-bit pools: times the value scale
+    float out_scale = 1.f;  // 8-bit pools: the value scale
     float k_scale = 1.f, v_scale = 1.f;  // 8-bit pools: the append stores E4M3(x / scale)
     // Calls that accumulate attention weights (instantiations with SCORES): every valid token's scores, in log2 units, as
     // [item][token of the chunk][head of the group] - see attn_finish_kernel.
@@ -700,6 +700,7 @@ __global__ void __launch_bounds__((NW + 1) * 32, KV8 ? 5 : 1)
 paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams p) {
     using SM = AttnSmem<D, STAGES, NW, KV8>;
     constexpr bool MB = BF16 && !KV8;  // the tensor-core products run in bf16 (else fp16: always so for 8-bit pools)
+    constexpr float P_SCALE = MB ? 1.f : ATT_P_SCALE_F16;
     static_assert(!KV8 || D == 128, "8-bit blocks: head_dim 128 (one 128-byte row per token)");
     // A stage must always be consumed by the same warp: tile i goes to warp i % NW and to stage i % STAGES.  If two
     // warps alternated on a stage, the one running ahead could pass a parity wait on the phase before the one it
@@ -1180,7 +1181,6 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                 }
             }
             // P^T as the B operand of O^T += V^T P^T: transpose the two 8x8 (token x head) blocks
-            constexpr float P_SCALE = MB ? 1.f : ATT_P_SCALE_F16;
             const uint32_t h01 = pack2<MB>(p0 * P_SCALE, p1 * P_SCALE), h23 = pack2<MB>(p2 * P_SCALE, p3 * P_SCALE);
             const uint32_t pb0 = movmatrix_trans(h01);
             const uint32_t pb1 = movmatrix_trans(h23);
@@ -1285,7 +1285,8 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                 acc += mo[(w * 8 + g) * SM::MO_STRIDE + d] * wt;
                 ll += ml[(w * 8 + g) * 2 + 1] * wt;
             }
-            acc *= p.out_scale;
+            acc *= 1.f / P_SCALE;    // (a factor of its own: together with a tiny value scale it would be subnormal)
+            acc *= p.out_scale;      // 1 for 16-bit pools
             if (it.nchunks == 1) {
                 // the whole context in one chunk: normalise and round here
                 const float r = acc * (ll > 0.f ? 1.f / ll : 0.f);
@@ -1786,7 +1787,6 @@ cudaError_t launch_attention(const AttnShape &sh, const AttnScratch &sc, const A
         p.v_scale = p.out_scale = a.v_scale;
         p.scale_log2e *= a.k_scale;  // scores over the stored keys are scores over the keys / k_scale
     }
-    if (sh.kv_fp8 || sh.dtype != PIE_BF16) p.out_scale *= 1.f / ATT_P_SCALE_F16;
     if (a.k_new == nullptr || a.v_new == nullptr) p.k_new = p.v_new = nullptr;
     if (a.weights != nullptr) {
         p.scores = sc.scores;

@@ -285,3 +285,18 @@ def test_evict_selection_over_several_pieces(in_place, name, budget, recent):
          "close": 1 + rng.integers(0, 5000, shape) * 2.0 ** -23}[name]
     with Pool(2, hkv, 64, F16, 1250 + (budget + 15) // 16, seqs=1) as p:
         EvictCase(p, [n], np.ascontiguousarray(w, dtype=np.float32), budget, recent, in_place, 350)
+
+
+def test_decode_with_a_tiny_value_scale():
+    """8-bit values times 2^-118, bf16: the outputs are those of the scale 1 times 2^-118 (what falls below 2^-126 may be 0)."""
+    n, hq, hkv, d = 300, 4, 2, 128
+    outs = []
+    for v_scale in (1.0, 2.0 ** -118):
+        with Pool(hq, hkv, d, BF16, (n + 15) // 16, fp8=True, seqs=1, v_scale=v_scale) as p:
+            p.fill(p.random(940))
+            tab, ctx, dq = up(np.arange(p.blocks, dtype=np.int32)[None]), up(np.array([n], np.int32)), up(rows(941, 1, hq, d, BF16))
+            out = torch.zeros_like(dq)
+            pie.pie_decode_attention(p.h, 0, dq.data_ptr(), out.data_ptr(), tab.data_ptr(), p.blocks, ctx.data_ptr(), 1, d ** -0.5)
+            pie.pie_sync(p.h)
+            outs.append(down(out, BF16))
+    assert np.abs(outs[0]).max() > 0.01 and np.all(np.abs(outs[1] - outs[0] * 2.0 ** -118) <= 2.0 ** -126)
