@@ -95,6 +95,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmap, const PrefillParam
     const uint32_t bar_k = base + SM::OFF_BAR, bar_v = bar_k + 16, bar_s = bar_k + 32, bar_o2 = bar_k + 48, bar_p = bar_k + 64;
     const uint32_t bar_p2[2] = {bar_p, bar_p + 8};
     const uint32_t bar_done = bar_k + 80;   // O is final (used once)
+    const uint32_t bar_end = bar_k + 88;    // where the CTA gives up: the MMAs issued by then are complete
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
 
     // ---- which tile
@@ -122,6 +123,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmap, const PrefillParam
         pf_mbar_init(bar_p2[0], PF_ROWS_THREADS);                      // P of a stage is in place: every row's thread arrives
         pf_mbar_init(bar_p2[1], PF_ROWS_THREADS);
         pf_mbar_init(bar_done, 1);
+        pf_mbar_init(bar_end, 1);
         misc[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -303,6 +305,11 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmap, const PrefillParam
                 if (j + 1 == n_stages) tc_commit(bar_done);   // O is final
             }
             __syncwarp();
+        }
+        if (dead()) {   // giving up: the MMAs in flight still read this CTA's shared memory and write its tensor memory
+            if (lane == 0) tc_commit(bar_end);
+            __syncwarp();
+            pf_mbar_wait(bar_end, 0u);
         }
         __syncwarp();
     } else {
@@ -519,6 +526,7 @@ prefill_attn_wide_kernel(const __grid_constant__ CUtensorMap tmap, const Prefill
     // CTA's warps do the softmax, the other's MMAs run.)
     const uint32_t bar_k = base + SM::OFF_BAR, bar_v = bar_k + 8, bar_s = bar_k + 16, bar_o = bar_k + 24, bar_p = bar_k + 32;
     const uint32_t bar_done = bar_k + 40;   // O is final (used once: the softmax warps do not follow bar_o)
+    const uint32_t bar_end = bar_k + 48;    // where the CTA gives up: the MMAs issued by then are complete
     volatile uint32_t *misc = reinterpret_cast<volatile uint32_t *>(smem + SM::OFF_MISC);
 
     // ---- which tile
@@ -545,6 +553,7 @@ prefill_attn_wide_kernel(const __grid_constant__ CUtensorMap tmap, const Prefill
         for (int i = 0; i < 4; ++i) pf_mbar_init(bar_k + 8 * i, 1);   // k_full, v_full, s_done, o_done
         pf_mbar_init(bar_p, PF_ROWS_THREADS);                          // P of a stage is in place: every row's thread arrives
         pf_mbar_init(bar_done, 1);
+        pf_mbar_init(bar_end, 1);
         misc[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -711,6 +720,11 @@ prefill_attn_wide_kernel(const __grid_constant__ CUtensorMap tmap, const Prefill
                 if (dead()) break;
                 issue_qk(j + 1);
             }
+        }
+        if (dead()) {   // giving up: the MMAs in flight still read this CTA's shared memory and write its tensor memory
+            if (lane == 0) tc_commit(bar_end);
+            __syncwarp();
+            pf_mbar_wait(bar_end, 0u);
         }
         __syncwarp();
     } else {
